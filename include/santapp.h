@@ -23,6 +23,10 @@
  *                         with the settings stated after it.
  *   santapp_build_teams_from_labels  Alg. "Build actual-key teams from a
  *                         parent partition" for any parent partition.
+ *   santapp_rope, santapp_rope_append, santapp_prompt_attention,
+ *   santapp_prefix_decode  what a decoder runs around these: rotary positions,
+ *                         the prompt's own attention, and exact decoding of
+ *                         several sequences over one prompt.
  *
  * Conventions
  *   - Every tensor argument is a DEVICE pointer owned by the caller unless
@@ -41,6 +45,11 @@
  *   - santapp_decode and santapp_dense_decode never allocate: the caller
  *     provides a workspace of the queried size, zeroed once before its
  *     first use.
+ *   - santapp_rope, santapp_rope_append, santapp_prompt_attention and
+ *     santapp_prefix_decode never allocate and never synchronise, and may be
+ *     captured into a HIP graph; their workspaces need no initialisation.
+ *     Calls that overlap in time (other streams, graphs replayed together)
+ *     need a workspace each.
  */
 #ifndef SANTAPP_H
 #define SANTAPP_H
@@ -374,6 +383,133 @@ santapp_status santapp_routing_kl_workspace_bytes(const santapp_teams* teams, in
  */
 santapp_status santapp_routing_kl(const santapp_teams* teams, const float* q, int Hq, double scale,
                                   double* kl, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Rows of a tensor [B][heads][tokens] of d contiguous elements each: the first
+ * row's address (16-byte aligned) and the distances between rows in elements
+ * (not negative; of a dimension of more than one entry, a multiple of 16 bytes).
+ * Inputs may repeat rows (distance 0), outputs may not share any.
+ */
+typedef struct {
+    void* data;
+    int64_t batch, head, token;
+} santapp_rows;
+
+/*
+ * A rotation by position.  With a = position * freqs[i] and i < pairs, the
+ * elements (x1, x2) of pair i become
+ *   magnitude (x1 cos a - x2 sin a),  magnitude (x2 cos a + x1 sin a);
+ * pair i is elements (i, i + pairs) of a row, or (2 i, 2 i + 1) when interleaved;
+ * the d - 2 pairs elements behind the pairs are copied.  Angles are formed in
+ * fp64, products in fp32, results rounded once.  Rotating by the negated
+ * positions (and 1 / magnitude) undoes a rotation; by the negated positions
+ * (and the same magnitude) it is the rotation's gradient.
+ */
+typedef struct {
+    const double* freqs; /* device [pairs], radians per position            */
+    int pairs;           /* 1 .. d / 2                                      */
+    int interleaved;     /* 0 or 1                                          */
+    double magnitude;    /* finite; a factor on sine and cosine             */
+} santapp_rotation;
+
+/*
+ * Rotate the rows x [B,H,T,d] into out [B,H,T,d] (types may differ; out may be
+ * x itself, and must otherwise not overlap it).  Token t of sequence b is at
+ * positions[b T + t] (device, any int32) or, with positions NULL, at first + t.
+ * Limits: d in {64, 128}.  T == 0 does nothing.
+ */
+santapp_status santapp_rope(const santapp_rotation* rotation, const santapp_rows* x, santapp_dtype x_dtype,
+                            int B, int H, int T, int d, const int* positions, int64_t first,
+                            const santapp_rows* out, santapp_dtype out_dtype, void* stream);
+
+/*
+ * One launch for T new tokens of every sequence: keys k [B,Hkv,T,d] rotated
+ * into rows at[b] + t of cache_K [B,Hkv,capacity,d], values v copied to the
+ * same rows of cache_V, and queries q [B,Hq,T,d] rotated into q_out (q NULL
+ * and Hq 0: none).  at: device [B], or NULL for at0 in every sequence; the caller
+ * advances it.  A token whose row lies outside [0, capacity) is not appended
+ * (its query is still rotated).  Token t is at positions[b T + t] or, with
+ * positions NULL, at first + at[b] + t (first: the prompt's length, say).
+ * q, k and v, and the caches, may be of either type; values are rounded when the
+ * caches' type is narrower.  The caches must not overlap the inputs.
+ */
+santapp_status santapp_rope_append(const santapp_rotation* rotation, const santapp_rows* q, santapp_dtype q_dtype,
+                                   const santapp_rows* q_out, santapp_dtype q_out_dtype, const santapp_rows* k,
+                                   const santapp_rows* v, santapp_dtype kv_dtype, const santapp_rows* cache_K,
+                                   const santapp_rows* cache_V, santapp_dtype cache_dtype, int capacity, int B,
+                                   int Hq, int Hkv, int T, int d, const int* at, int at0, const int* positions,
+                                   int64_t first, void* stream);
+
+/*
+ * How the two calls below form the score of a query at position p and a key at
+ * position j:  s = scale q.k;  with softcap > 0, s = softcap tanh(s / softcap);
+ * with slopes, s -= slopes[h] |p - j|.  With window > 0 only keys with
+ * |p - j| < window are attended.
+ */
+typedef struct {
+    double scale;        /* 0: 1 / sqrt(d)                      */
+    double softcap;      /* 0: none                             */
+    const float* slopes; /* device [Hq], or NULL                */
+    int window;          /* 0: none                             */
+} santapp_score;
+
+/*
+ * Workspace of santapp_prompt_attention with these sizes (bytes, host-only
+ * query; 0 for most large calls); documents: whether the call has them.
+ */
+santapp_status santapp_prompt_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int d, santapp_dtype dtype,
+                                              int window, int documents, size_t* bytes);
+
+/*
+ * Softmax attention of the query tokens q [B,Hq,T,d] over the keys and values
+ * K, V [B,Hkv,N,d] of the same type; query head h reads KV head h / (Hq / Hkv),
+ * key j is at position j and query token t at offset + t (offset N - T: the last
+ * T tokens of the sequence).  Key j is attended when
+ *   causal is 0, or j <= offset + t, or prefix is given and j < prefix[b]; and
+ *   |offset + t - j| < window (window > 0); and
+ *   documents [B,N] is NULL, or token j's document equals the query token's and
+ *   is not negative (negative: padding).
+ * out [B,Hq,T,d], of the same type; a query without any key gets 0.  documents
+ * and prefix are device int32.  Scores, weights' sums and value sums are fp32;
+ * bf16 calls round the weights to bf16 for the product with V.
+ * The queries must be tokens of the sequence (0 <= offset, offset + T <= N)
+ * unless causal, window, slopes and documents are all absent.  Keys that no
+ * query of a block of up to 128 (token, head) rows attends, padding and others,
+ * are not read or count for nothing whatever they hold; a NaN or infinity in V
+ * reaches the outputs that attend it and no other.
+ * Limits: d in {64, 128}, N < 2^24, T Hq / Hkv < 2^30; rows of K and V at
+ * most 64 MiB apart.
+ */
+santapp_status santapp_prompt_attention(const santapp_score* score, const santapp_rows* q, const santapp_rows* K,
+                                        const santapp_rows* V, santapp_dtype dtype, int B, int Hq, int Hkv, int T,
+                                        int N, int d, int causal, int offset, const int* documents,
+                                        const int* prefix, const santapp_rows* out, void* workspace,
+                                        size_t ws_bytes, void* stream);
+
+/* Workspace of santapp_prefix_decode with these sizes (bytes, host-only query). */
+santapp_status santapp_prefix_workspace_bytes(int P, int S, int Hq, int Hkv, int N, int T, int d,
+                                              santapp_dtype dtype, size_t* bytes);
+
+/*
+ * One exact decode step of S sequences over each of P prompts: sequence b
+ * (of P S) attends the first prefix_lengths[p] rows of prompt p = b / S in
+ * K, V [P,Hkv,N,d] and the first lengths[b] rows of its own suffix_K,
+ * suffix_V [P S,Hkv,T,d].  A prompt's rows are read once for all its sequences.
+ * prefix_lengths [P] and lengths [P S] are device int32, clamped to [0, N] and
+ * [0, T]; NULL means N and T.  Rows behind a length are not attended whatever
+ * they hold.  For slopes and windows, prompt row j is at position j, suffix row t at
+ * prefix_lengths[p] + t and the query at positions[b] (device int32) or, with
+ * positions NULL, at the sequence's last row.
+ * q, out: fp32 [P S,Hq,d], dense.  A query without any row gets 0.  S = 1 is
+ * an ordinary dense step.  Limits: d in {64, 128}, N and T < 2^24, P S Hq <
+ * 2^22; key and value rows at most 64 MiB apart.
+ */
+santapp_status santapp_prefix_decode(const santapp_score* score, const float* q, const santapp_rows* K,
+                                     const santapp_rows* V, santapp_dtype dtype, int P, int S, int Hq, int Hkv,
+                                     int N, int d, const int* prefix_lengths, const santapp_rows* suffix_K,
+                                     const santapp_rows* suffix_V, int T, const int* lengths,
+                                     const int* positions, float* out, void* workspace, size_t ws_bytes,
+                                     void* stream);
 
 /* Message of the last failed call on this thread ("" if none). */
 const char* santapp_last_error(void);

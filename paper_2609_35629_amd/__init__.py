@@ -14,9 +14,12 @@ import torch
 
 from . import _lib
 from ._lib import SantappError, check  # noqa: F401
+from .attention import (prefix_decode, prefix_workspace, prompt_attention, prompt_workspace, rope,  # noqa: F401
+                        rope_append, rope_frequencies)
 
 __all__ = ["Teams", "build_teams", "decode", "decode_static", "dense_decode", "decode_workspace",
-           "dense_workspace", "budget_to_K", "trim", "SantappError"]
+           "dense_workspace", "budget_to_K", "trim", "SantappError", "rope", "rope_append", "rope_frequencies",
+           "prompt_attention", "prompt_workspace", "prefix_decode", "prefix_workspace"]
 
 
 def _dtype_code(t: torch.Tensor) -> int:

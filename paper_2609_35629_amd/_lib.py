@@ -20,7 +20,8 @@ EXPORTS = [
     "santapp_dense_workspace_bytes", "santapp_dense_decode", "santapp_last_error",
     "santapp_teams_set_route_keys", "santapp_routing_kl_workspace_bytes", "santapp_routing_kl",
     "santapp_kmeans_parents", "santapp_build_teams_from_labels", "santapp_decode_launch_info",
-    "santapp_trim",
+    "santapp_trim", "santapp_rope", "santapp_rope_append", "santapp_prompt_workspace_bytes",
+    "santapp_prompt_attention", "santapp_prefix_workspace_bytes", "santapp_prefix_decode",
 ]
 
 ROUTE_REPRESENTATIVE, ROUTE_CENTROID = 0, 1
@@ -51,6 +52,21 @@ class DecodeDebug(ctypes.Structure):
         ("logc", ctypes.c_void_p), ("tau", ctypes.c_void_p), ("union_teams", ctypes.c_void_p),
         ("union_rows", ctypes.c_void_p), ("events", ctypes.c_void_p * 4),
     ]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("head", ctypes.c_int64),
+                ("token", ctypes.c_int64)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("freqs", ctypes.c_void_p), ("pairs", ctypes.c_int), ("interleaved", ctypes.c_int),
+                ("magnitude", ctypes.c_double)]
+
+
+class Score(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_double), ("softcap", ctypes.c_double), ("slopes", ctypes.c_void_p),
+                ("window", ctypes.c_int)]
 
 
 class SantappError(RuntimeError):
@@ -95,6 +111,16 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     L.santapp_teams_set_route_keys.argtypes = [vp, i, vp]
     L.santapp_routing_kl_workspace_bytes.argtypes = [vp, i, ctypes.POINTER(sz)]
     L.santapp_routing_kl.argtypes = [vp, vp, i, ctypes.c_double, vp, vp, sz, vp]
+    rows, i64 = ctypes.POINTER(Rows), ctypes.c_int64
+    rotation, score = ctypes.POINTER(Rotation), ctypes.POINTER(Score)
+    L.santapp_rope.argtypes = [rotation, rows, i, i, i, i, i, vp, i64, rows, i, vp]
+    L.santapp_rope_append.argtypes = [rotation, rows, i, rows, i, rows, rows, i, rows, rows, i, i, i, i, i, i, i, vp,
+                                      i, vp, i64, vp]
+    L.santapp_prompt_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i, i, ctypes.POINTER(sz)]
+    L.santapp_prompt_attention.argtypes = [score, rows, rows, rows, i, i, i, i, i, i, i, i, i, vp, vp, rows, vp, sz, vp]
+    L.santapp_prefix_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i, ctypes.POINTER(sz)]
+    L.santapp_prefix_decode.argtypes = [score, vp, rows, rows, i, i, i, i, i, i, i, vp, rows, rows, i, vp, vp, vp, vp,
+                                        sz, vp]
     L.santapp_last_error.argtypes = []
     L.santapp_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:

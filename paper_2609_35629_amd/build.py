@@ -15,7 +15,7 @@ OBJDIR = os.path.join(ROOT, "_build", "santapp")
 LIB = os.path.join(PKG, "libsantapp.so")
 PROBE_LIB = os.path.join(PKG, "libsantapp_probe.so")  # streaming-read probe (measurement only)
 SOURCES = ["api.hip", "build_kernels.hip", "route_kernels.hip", "decode_kernels.hip", "diag_kernels.hip",
-           "kmeans_kernels.hip"]
+           "kmeans_kernels.hip", "rope_kernels.hip", "prompt_kernels.hip", "prefix_kernels.hip"]
 
 ARCH = os.environ.get("SANTAPP_ARCH", "gfx950")
 CFLAGS = [

@@ -487,6 +487,111 @@ StepLayout dense_layout(int B, int Hq, int Hkv, int N, int T, int d, int cus, sa
 
 using namespace santapp;
 
+namespace {
+
+// A view of B x heads x tokens rows of d elements as the kernels take it
+// (distances in bytes, 0 along dimensions of one entry).  `out`: no two rows
+// may share bytes.
+santapp_status check_rows(const santapp_rows* v, const char* name, santapp_dtype dt, long long B, long long H,
+                          long long T, int d, bool out, Rows* r) {
+    if (!v || !v->data) return fail(SANTAPP_EINVAL, "%s is NULL", name);
+    if (!aligned16(v->data)) return fail(SANTAPP_EINVAL, "%s must be 16-byte aligned", name);
+    const long long es = static_cast<long long>(elem_size(dt));
+    struct Dim {
+        long long n, stride;
+    } dim[3] = {{B, v->batch}, {H, v->head}, {T, v->token}};
+    for (Dim& x : dim) {
+        if (x.n <= 1) x.stride = 0;
+        if (x.stride < 0 || x.stride % (16 / es) != 0 || x.stride > (1ll << 48))
+            return fail(SANTAPP_EINVAL, "%s: distances between rows must be multiples of 16 bytes and not negative", name);
+    }
+    r->p = static_cast<const char*>(v->data);
+    r->b = dim[0].stride * es;
+    r->h = dim[1].stride * es;
+    r->t = dim[2].stride * es;
+    if (out) {
+        std::sort(dim, dim + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+        long long extent = d;  // elements from the first to the end of the last row so far
+        for (const Dim& x : dim) {
+            if (x.n <= 1) continue;
+            if (x.stride < extent) return fail(SANTAPP_EINVAL, "%s: rows overlap", name);
+            extent += (x.n - 1) * x.stride;
+        }
+    }
+    return SANTAPP_OK;
+}
+
+// Keys or values: rows within the reach of the kernels' offsets.
+santapp_status check_keys(const santapp_rows* v, const char* name, santapp_dtype dt, long long B, long long H, long long T,
+                          int d, Rows* r) {
+    if (santapp_status st = check_rows(v, name, dt, B, H, T, d, false, r)) return st;
+    if (r->t > kMaxRowStep) return fail(SANTAPP_ELIMIT, "%s: rows more than %lld bytes apart", name, kMaxRowStep);
+    return SANTAPP_OK;
+}
+
+santapp_status check_score(const santapp_score* sc, int d, ScoreArgs* a) {
+    if (!sc) return fail(SANTAPP_EINVAL, "score is NULL");
+    double scale = sc->scale;
+    if (!(scale >= 0.0) || !isfinite(scale)) return fail(SANTAPP_EINVAL, "scale must be finite and >= 0");
+    if (scale == 0.0) scale = 1.0 / sqrt(static_cast<double>(d));
+    if (!(sc->softcap >= 0.0) || !isfinite(sc->softcap)) return fail(SANTAPP_EINVAL, "softcap must be finite and >= 0");
+    if (sc->window < 0) return fail(SANTAPP_EINVAL, "window must be >= 0");
+    constexpr double log2e = 1.4426950408889634;
+    // every factor has to be an ordinary fp32 number
+    auto fits = [](double x) { return x >= 1e-30 && x <= 1e30; };
+    if (!fits(scale) || (sc->softcap > 0.0 && (!fits(sc->softcap) || !fits(scale / sc->softcap))))
+        return fail(SANTAPP_EINVAL, "scale and softcap must lie in [1e-30, 1e30]");
+    a->scale_log2 = static_cast<float>(scale * log2e);
+    a->capped = sc->softcap > 0.0;
+    a->inv_cap = a->capped ? static_cast<float>(scale / sc->softcap) : 0.f;
+    a->cap_log2 = static_cast<float>(sc->softcap * log2e);
+    a->slopes = sc->slopes;
+    a->window = sc->window;
+    return SANTAPP_OK;
+}
+
+santapp_status check_head_dim(int d) {
+    if (d != 64 && d != 128) return fail(SANTAPP_ELIMIT, "head dim %d not supported (64 or 128)", d);
+    return SANTAPP_OK;
+}
+
+santapp_status check_rotation(const santapp_rotation* r, int d) {
+    if (!r || !r->freqs) return fail(SANTAPP_EINVAL, "rotation and its freqs must be given");
+    if (reinterpret_cast<uintptr_t>(r->freqs) % 8 != 0) return fail(SANTAPP_EINVAL, "freqs must be 8-byte aligned");
+    if (r->pairs < 1 || r->pairs > d / 2) return fail(SANTAPP_EINVAL, "pairs must be in 1 .. d / 2");
+    if (r->interleaved != 0 && r->interleaved != 1) return fail(SANTAPP_EINVAL, "interleaved must be 0 or 1");
+    if (!isfinite(r->magnitude)) return fail(SANTAPP_EINVAL, "magnitude must be finite");
+    return SANTAPP_OK;
+}
+
+// Device int32 arrays: aligned as such.
+bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
+
+RopeStream rope_stream(const Rows& in, santapp_dtype in_dt, const Rows& out, santapp_dtype out_dt, int heads, bool rotate,
+                       bool append) {
+    const long long ie = static_cast<long long>(elem_size(in_dt)), oe = static_cast<long long>(elem_size(out_dt));
+    RopeStream s{};
+    s.in = in.p;
+    s.out = const_cast<char*>(out.p);
+    s.ib = in.b / ie;
+    s.ih = in.h / ie;
+    s.it = in.t / ie;
+    s.ob = out.b / oe;
+    s.oh = out.h / oe;
+    s.ot = out.t / oe;
+    s.heads = heads;
+    s.in32 = in_dt == SANTAPP_FP32;
+    s.out32 = out_dt == SANTAPP_FP32;
+    s.rotate = rotate;
+    s.append = append;
+    return s;
+}
+
+constexpr long long kMaxRows = 1ll << 30;   // (token, head) rows of a call's grid
+constexpr int kMaxKeys = 1 << 24;           // positions exact in fp32
+
+}  // namespace
+
 extern "C" {
 
 const char* santapp_last_error(void) { return g_err.c_str(); }
@@ -1147,6 +1252,212 @@ santapp_status santapp_dense_decode(const float* q, const void* K, const void* V
     if ((e = launch_decode(A, s)) != hipSuccess) return hip_fail(e, "dense decode kernels");
     if ((e = mark(3)) != hipSuccess) return hip_fail(e, "event record");
     return ok();
+}
+
+santapp_status santapp_rope(const santapp_rotation* rotation, const santapp_rows* x, santapp_dtype x_dtype, int B,
+                            int H, int T, int d, const int* positions, int64_t first, const santapp_rows* out,
+                            santapp_dtype out_dtype, void* stream) {
+    if (B < 1 || H < 1 || T < 0) return fail(SANTAPP_EINVAL, "invalid sizes");
+    if (!dtype_ok(x_dtype) || !dtype_ok(out_dtype)) return fail(SANTAPP_EDTYPE, "unsupported dtype");
+    if (santapp_status st = check_head_dim(d)) return st;
+    if (santapp_status st = check_rotation(rotation, d)) return st;
+    if (!aligned4(positions)) return fail(SANTAPP_EINVAL, "positions must be 4-byte aligned");
+    if (T == 0) return ok();
+    if (static_cast<long long>(B) * T > kMaxRows || static_cast<long long>(B) * T * H > 8 * kMaxRows)
+        return fail(SANTAPP_ELIMIT, "too many rows");
+    Rows xr, yr;
+    if (santapp_status st = check_rows(x, "x", x_dtype, B, H, T, d, false, &xr)) return st;
+    if (santapp_status st = check_rows(out, "out", out_dtype, B, H, T, d, true, &yr)) return st;
+    RopeArgs a{};
+    a.s[0] = rope_stream(xr, x_dtype, yr, out_dtype, H, true, false);
+    a.freqs = rotation->freqs;
+    a.positions = positions;
+    a.first = first;
+    a.capacity = T;
+    a.pairs = rotation->pairs;
+    a.B = B;
+    a.T = T;
+    a.d = d;
+    a.magnitude = static_cast<float>(rotation->magnitude);
+    a.interleaved = rotation->interleaved != 0;
+    const hipError_t e = launch_rope(a, device_cus(), static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ok() : hip_fail(e, "rotation kernel");
+}
+
+santapp_status santapp_rope_append(const santapp_rotation* rotation, const santapp_rows* q, santapp_dtype q_dtype,
+                                   const santapp_rows* q_out, santapp_dtype q_out_dtype, const santapp_rows* k,
+                                   const santapp_rows* v, santapp_dtype kv_dtype, const santapp_rows* cache_K,
+                                   const santapp_rows* cache_V, santapp_dtype cache_dtype, int capacity, int B,
+                                   int Hq, int Hkv, int T, int d, const int* at, int at0, const int* positions,
+                                   int64_t first, void* stream) {
+    if (B < 1 || Hkv < 1 || Hq < 0 || T < 0 || capacity < 1) return fail(SANTAPP_EINVAL, "invalid sizes");
+    if ((q != nullptr) != (Hq > 0)) return fail(SANTAPP_EINVAL, "q must be given with Hq > 0, and NULL with Hq == 0");
+    if (!dtype_ok(kv_dtype) || !dtype_ok(cache_dtype) || (q && (!dtype_ok(q_dtype) || !dtype_ok(q_out_dtype))))
+        return fail(SANTAPP_EDTYPE, "unsupported dtype");
+    if (santapp_status st = check_head_dim(d)) return st;
+    if (santapp_status st = check_rotation(rotation, d)) return st;
+    if (!aligned4(positions) || !aligned4(at)) return fail(SANTAPP_EINVAL, "positions and at must be 4-byte aligned");
+    if (!at && (at0 < 0 || static_cast<long long>(at0) + T > capacity))
+        return fail(SANTAPP_EINVAL, "rows %d .. %lld outside the cache's %d", at0, static_cast<long long>(at0) + T, capacity);
+    if (T == 0) return ok();
+    if (static_cast<long long>(B) * T > kMaxRows || static_cast<long long>(B) * T * (Hq + 2ll * Hkv) > 8 * kMaxRows)
+        return fail(SANTAPP_ELIMIT, "too many rows");
+    Rows qr, qo, kr, vr, ck, cv;
+    RopeArgs a{};
+    if (q) {
+        if (santapp_status st = check_rows(q, "q", q_dtype, B, Hq, T, d, false, &qr)) return st;
+        if (santapp_status st = check_rows(q_out, "q_out", q_out_dtype, B, Hq, T, d, true, &qo)) return st;
+        a.s[0] = rope_stream(qr, q_dtype, qo, q_out_dtype, Hq, true, false);
+    }
+    if (santapp_status st = check_rows(k, "k", kv_dtype, B, Hkv, T, d, false, &kr)) return st;
+    if (santapp_status st = check_rows(v, "v", kv_dtype, B, Hkv, T, d, false, &vr)) return st;
+    if (santapp_status st = check_rows(cache_K, "cache_K", cache_dtype, B, Hkv, capacity, d, true, &ck)) return st;
+    if (santapp_status st = check_rows(cache_V, "cache_V", cache_dtype, B, Hkv, capacity, d, true, &cv)) return st;
+    a.s[1] = rope_stream(kr, kv_dtype, ck, cache_dtype, Hkv, true, true);
+    a.s[2] = rope_stream(vr, kv_dtype, cv, cache_dtype, Hkv, false, true);
+    a.freqs = rotation->freqs;
+    a.positions = positions;
+    a.at = at;
+    a.at0 = at0;
+    a.first = first;
+    a.capacity = capacity;
+    a.pairs = rotation->pairs;
+    a.B = B;
+    a.T = T;
+    a.d = d;
+    a.magnitude = static_cast<float>(rotation->magnitude);
+    a.interleaved = rotation->interleaved != 0;
+    const hipError_t e = launch_rope(a, device_cus(), static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ok() : hip_fail(e, "rotation kernel");
+}
+
+static santapp_status prompt_sizes(int B, int Hq, int Hkv, int T, int N, int d, santapp_dtype dtype, PromptArgs* a) {
+    if (B < 1 || Hkv < 1 || T < 0 || N < 0) return fail(SANTAPP_EINVAL, "invalid sizes");
+    if (Hq < 1 || Hq % Hkv != 0) return fail(SANTAPP_EINVAL, "Hq must be a positive multiple of Hkv");
+    if (!dtype_ok(dtype)) return fail(SANTAPP_EDTYPE, "unsupported dtype %d", static_cast<int>(dtype));
+    if (santapp_status st = check_head_dim(d)) return st;
+    if (N >= kMaxKeys) return fail(SANTAPP_ELIMIT, "N must be below 2^24");
+    if (static_cast<long long>(T) * (Hq / Hkv) >= kMaxRows || static_cast<long long>(T) * Hq * B / 32 >= kMaxRows)
+        return fail(SANTAPP_ELIMIT, "too many rows");
+    a->B = B;
+    a->Hkv = Hkv;
+    a->G = Hq / Hkv;
+    a->T = T;
+    a->N = N;
+    a->d = d;
+    a->dtype = dtype;
+    return SANTAPP_OK;
+}
+
+santapp_status santapp_prompt_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int d, santapp_dtype dtype,
+                                              int window, int documents, size_t* bytes) {
+    if (!bytes) return fail(SANTAPP_EINVAL, "bytes is NULL");
+    if (window < 0) return fail(SANTAPP_EINVAL, "window must be >= 0");
+    PromptArgs a{};
+    if (santapp_status st = prompt_sizes(B, Hq, Hkv, T, N, d, dtype, &a)) return st;
+    static const int some = 0;
+    a.documents = documents ? &some : nullptr;
+    a.score.window = window;
+    *bytes = T == 0 ? 0 : plan_prompt(a, device_cus(), nullptr);
+    return ok();
+}
+
+santapp_status santapp_prompt_attention(const santapp_score* score, const santapp_rows* q, const santapp_rows* K,
+                                        const santapp_rows* V, santapp_dtype dtype, int B, int Hq, int Hkv, int T,
+                                        int N, int d, int causal, int offset, const int* documents,
+                                        const int* prefix, const santapp_rows* out, void* workspace,
+                                        size_t ws_bytes, void* stream) {
+    PromptArgs a{};
+    if (santapp_status st = prompt_sizes(B, Hq, Hkv, T, N, d, dtype, &a)) return st;
+    if (santapp_status st = check_score(score, d, &a.score)) return st;
+    if (causal != 0 && causal != 1) return fail(SANTAPP_EINVAL, "causal must be 0 or 1");
+    if (prefix && !causal) return fail(SANTAPP_EINVAL, "a prefix needs causal");
+    if (!aligned4(documents) || !aligned4(prefix) || !aligned4(score->slopes))
+        return fail(SANTAPP_EINVAL, "documents, prefix and slopes must be 4-byte aligned");
+    if ((causal || score->window > 0 || score->slopes || documents) &&
+        (offset < 0 || static_cast<long long>(offset) + T > N))
+        return fail(SANTAPP_EINVAL, "queries %d .. %lld are not tokens of the sequence's %d", offset,
+                    static_cast<long long>(offset) + T, N);
+    if (T == 0) return ok();
+    if (santapp_status st = check_rows(q, "q", dtype, B, Hq, T, d, false, &a.q)) return st;
+    if (santapp_status st = check_rows(out, "out", dtype, B, Hq, T, d, true, &a.out)) return st;
+    if (N > 0) {
+        if (santapp_status st = check_keys(K, "K", dtype, B, Hkv, N, d, &a.K)) return st;
+        if (santapp_status st = check_keys(V, "V", dtype, B, Hkv, N, d, &a.V)) return st;
+    }
+    a.causal = causal != 0;
+    a.offset = offset;
+    a.documents = documents;
+    a.prefix = prefix;
+    if (!aligned16(workspace)) return fail(SANTAPP_EINVAL, "workspace must be 16-byte aligned");
+    const size_t need = plan_prompt(a, device_cus(), static_cast<char*>(workspace));
+    if (need > 0 && (!workspace || ws_bytes < need))
+        return fail(SANTAPP_EWORKSPACE, "workspace of %zu bytes needed (got %zu)", need, workspace ? ws_bytes : 0);
+    const hipError_t e = launch_prompt(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ok() : hip_fail(e, "prompt attention kernels");
+}
+
+static santapp_status prefix_sizes(int P, int S, int Hq, int Hkv, int N, int T, int d, santapp_dtype dtype,
+                                   PrefixArgs* a) {
+    if (P < 1 || S < 1 || Hkv < 1 || T < 0 || N < 0) return fail(SANTAPP_EINVAL, "invalid sizes");
+    if (Hq < 1 || Hq % Hkv != 0) return fail(SANTAPP_EINVAL, "Hq must be a positive multiple of Hkv");
+    if (!dtype_ok(dtype)) return fail(SANTAPP_EDTYPE, "unsupported dtype %d", static_cast<int>(dtype));
+    if (santapp_status st = check_head_dim(d)) return st;
+    if (N >= kMaxKeys || T >= kMaxKeys) return fail(SANTAPP_ELIMIT, "N and T must be below 2^24");
+    if (static_cast<long long>(P) * S * Hq >= (1 << 22)) return fail(SANTAPP_ELIMIT, "too many rows");
+    a->P = P;
+    a->S = S;
+    a->Hkv = Hkv;
+    a->G = Hq / Hkv;
+    a->N = N;
+    a->T = T;
+    a->d = d;
+    a->dtype = dtype;
+    return SANTAPP_OK;
+}
+
+santapp_status santapp_prefix_workspace_bytes(int P, int S, int Hq, int Hkv, int N, int T, int d,
+                                              santapp_dtype dtype, size_t* bytes) {
+    if (!bytes) return fail(SANTAPP_EINVAL, "bytes is NULL");
+    PrefixArgs a{};
+    if (santapp_status st = prefix_sizes(P, S, Hq, Hkv, N, T, d, dtype, &a)) return st;
+    *bytes = plan_prefix(a, device_cus(), nullptr);
+    return ok();
+}
+
+santapp_status santapp_prefix_decode(const santapp_score* score, const float* q, const santapp_rows* K,
+                                     const santapp_rows* V, santapp_dtype dtype, int P, int S, int Hq, int Hkv,
+                                     int N, int d, const int* prefix_lengths, const santapp_rows* suffix_K,
+                                     const santapp_rows* suffix_V, int T, const int* lengths,
+                                     const int* positions, float* out, void* workspace, size_t ws_bytes,
+                                     void* stream) {
+    if (!q || !out) return fail(SANTAPP_EINVAL, "q and out must be device pointers");
+    if (!aligned16(q) || !aligned16(out) || !aligned16(workspace))
+        return fail(SANTAPP_EINVAL, "q, out and workspace must be 16-byte aligned");
+    PrefixArgs a{};
+    if (santapp_status st = prefix_sizes(P, S, Hq, Hkv, N, T, d, dtype, &a)) return st;
+    if (santapp_status st = check_score(score, d, &a.score)) return st;
+    if (!aligned4(prefix_lengths) || !aligned4(lengths) || !aligned4(positions) || !aligned4(score->slopes))
+        return fail(SANTAPP_EINVAL, "lengths, positions and slopes must be 4-byte aligned");
+    const long long B = static_cast<long long>(P) * S;
+    if (N > 0) {
+        if (santapp_status st = check_keys(K, "K", dtype, P, Hkv, N, d, &a.K)) return st;
+        if (santapp_status st = check_keys(V, "V", dtype, P, Hkv, N, d, &a.V)) return st;
+    }
+    if (T > 0) {
+        if (santapp_status st = check_keys(suffix_K, "suffix_K", dtype, B, Hkv, T, d, &a.sK)) return st;
+        if (santapp_status st = check_keys(suffix_V, "suffix_V", dtype, B, Hkv, T, d, &a.sV)) return st;
+    }
+    a.q = q;
+    a.out = out;
+    a.prefix_lengths = prefix_lengths;
+    a.lengths = lengths;
+    a.positions = positions;
+    const size_t need = plan_prefix(a, device_cus(), static_cast<char*>(workspace));
+    if (need > 0 && (!workspace || ws_bytes < need))
+        return fail(SANTAPP_EWORKSPACE, "workspace of %zu bytes needed (got %zu)", need, workspace ? ws_bytes : 0);
+    const hipError_t e = launch_prefix(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ok() : hip_fail(e, "shared-prefix decode kernels");
 }
 
 }  // extern "C"

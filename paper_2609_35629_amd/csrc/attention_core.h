@@ -1,0 +1,634 @@
+// Softmax attention of blocks of query rows over tiles of key rows, on the
+// matrix cores; the device code shared by prompt attention and shared-prefix
+// decoding.
+//
+// The query rows of one (sequence, KV head) pair are its tokens' G heads, token
+// by token (row r: token r / G, head r % G), so that a block of rows reads each
+// key tile once for all of them.  A workgroup of WR x WK waves takes 32 WR rows
+// and walks the key tiles in one pass (running maximum m and sum l, in fp32 and
+// base 2):  S^T = K Q^T, P = 2^(s - m), O^T += V^T P^T.  The scores are formed
+// transposed so that a lane holds scores of one query row (column lane % 32 of the
+// 32 x 32 product, keys 8 (i / 4) + 4 (lane / 32) + i % 4 in register i): row
+// maxima and sums stay in the lane but for one exchange with the other half of
+// the wave, and P^T is the next product's right operand as it stands, once V's
+// rows are read in that key order.
+//
+// K and V tiles are copied to LDS by DMA (no registers), one tile ahead; their
+// 16-byte pieces are permuted within the row so that both the row reads of K
+// and the transposing reads of V spread over all banks.
+//
+// bf16 rows: v_mfma_f32_32x32x16_bf16.  fp32 queries over bf16 rows enter as
+// three bf16 terms each (q and P: 24 bits), so that the result is as exact as
+// fp32 products; bf16 queries as one, with P rounded to bf16 (2^-9, like the
+// output's own rounding).  fp32 rows: v_mfma_f32_32x32x2_f32.
+#pragma once
+
+#include "common.h"
+#include "internal.h"
+
+#include <type_traits>
+
+namespace santapp {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// One stretch of keys: rows K, V of n keys.
+struct KeySeg {
+    const char *K, *V;
+    long long kt, vt;  // bytes between rows, at most kMaxRowStep
+    int n;
+};
+
+// What one query row may attend: keys [lo, hi) of the stretch, of its document;
+// pos: its position relative to the stretch's first key; slope: log2(e) times
+// the bias per key of distance.
+struct RowInfo {
+    int lo, hi, pos, doc;
+    float slope;
+    bool valid;
+};
+
+// A lane's offset within a group of at most 32 rows has 32 bits.
+static_assert(32 * kMaxRowStep <= (1ll << 32), "");
+
+constexpr float kNegInf = -__builtin_inff();
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Value of the other half-wave's lane (lane ^ 32).
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+__device__ __forceinline__ int wave_min_i32(int v) {
+#pragma unroll
+    for (int k = 1; k < kWave; k *= 2) v = min(v, __shfl_xor(v, k));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int wave_max_i32(int v) {
+#pragma unroll
+    for (int k = 1; k < kWave; k *= 2) v = max(v, __shfl_xor(v, k));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+// tanh: 1 - 2 / (1 + e^2|y|) (absolute error about 2^-23), and where that would
+// cancel (|y| < 0.35; EXACT only) its Taylor series to y^13.
+template <bool EXACT>
+__device__ __forceinline__ float tanh_of(float y) {
+    const float a = fabsf(y);
+    float r = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + exp2_fast(a * 2.88539008177792681f));
+    if constexpr (EXACT) {
+        const float z = a * a;
+        const float t = a + a * z * (-1.f / 3 + z * (2.f / 15 + z * (-17.f / 315 + z * (62.f / 2835 +
+                                     z * (-1382.f / 155925 + z * (21844.f / 6081075))))));
+        r = a < 0.35f ? t : r;
+    }
+    return copysignf(r, y);
+}
+
+// Bytes of a row and the permutation of its 16-byte pieces: 16 rows at the
+// same piece, and 4 rows at 4 neighbouring pieces, fall into distinct banks.
+template <typename T, int D>
+struct Tile {
+    static constexpr int RB = D * static_cast<int>(sizeof(T));
+    static constexpr int SPR = RB / 16;
+    static __device__ __forceinline__ int perm(int row) {
+        if constexpr (RB >= 256)
+            return ((row & 3) << 2) | ((row >> 2) & 3);
+        else  // two rows share the 256 bytes of the banks
+            return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+    }
+    static __device__ __forceinline__ int at(int row, int byte) {
+        return row * RB + (((byte >> 4) ^ perm(row)) << 4) + (byte & 15);
+    }
+};
+
+// Query rows as right operands, scores and value sums of 32 keys.
+template <typename T, int D, int NT>
+struct Ops;
+
+template <int D, int NT>
+struct Ops<bf16_t, D, NT> {
+    using TL = Tile<bf16_t, D>;
+    bf16x8 q[NT][D / 16];
+
+    // NT == 1: bf16 query rows, else fp32 rows
+    __device__ __forceinline__ void load_q(const char* row, int hh) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            if constexpr (NT == 1) {
+                q[0][k] = *reinterpret_cast<const bf16x8*>(row + 2 * (16 * k + 8 * hh));
+            } else {
+                const float4* p = reinterpret_cast<const float4*>(row + 4 * (16 * k + 8 * hh));
+                const float4 u = p[0], v = p[1];
+                const float x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) split(x[e], k, e);
+            }
+        }
+    }
+    __device__ __forceinline__ void split(float x, int k, int e) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const __bf16 h = static_cast<__bf16>(x);
+            q[t][k][e] = h;
+            x -= static_cast<float>(h);
+        }
+    }
+    __device__ __forceinline__ f32x16 scores(const char* ktile, int row0, int lane) const {
+        f32x16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        const int row = row0 + (lane & 31), hh = lane >> 5;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            const bf16x8 a = *reinterpret_cast<const bf16x8*>(ktile + TL::at(row, 16 * (2 * k + hh)));
+#pragma unroll
+            for (int t = NT - 1; t >= 0; --t) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[t][k], s, 0, 0, 0);
+        }
+        return s;
+    }
+    // V^T of 4 keys x 16 dims per 16 lanes: lane s % 16 addresses key s / 4,
+    // dims 4 (s % 4) .. + 4, lane n receives the four keys of dim n.
+    static __device__ __forceinline__ bf16x8 values(const char* vtile, int row0, int db, int lane) {
+        typedef short v4i16 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+        const int s = lane & 15;
+        const int row = row0 + 4 * (lane >> 5) + (s >> 2);
+        const int byte = 64 * db + 32 * ((lane >> 4) & 1) + 8 * (s & 3);
+        const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vtile + TL::at(row, byte)));
+        const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vtile + TL::at(row + 8, byte)));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    static __device__ __forceinline__ void add_values(const char* vtile, int row0, const f32x16& p, f32x16 (&o)[D / 32],
+                                                      int lane) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            bf16x8 b[NT];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float x = p[8 * k + e];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const __bf16 h = static_cast<__bf16>(x);
+                    b[t][e] = h;
+                    x -= static_cast<float>(h);
+                }
+            }
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db) {
+                const bf16x8 a = values(vtile, row0 + 16 * k, db, lane);
+#pragma unroll
+                for (int t = NT - 1; t >= 0; --t)
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b[t], o[db], 0, 0, 0);
+            }
+        }
+    }
+};
+
+template <int D>
+struct Ops<float, D, 1> {
+    using TL = Tile<float, D>;
+    // dims 8 c + 4 (lane / 32) + e of the row, as q[c].e
+    float4 q[D / 8];
+
+    __device__ __forceinline__ void load_q(const char* row, int hh) {
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) q[c] = *reinterpret_cast<const float4*>(row + 4 * (8 * c + 4 * hh));
+    }
+    __device__ __forceinline__ f32x16 scores(const char* ktile, int row0, int lane) const {
+        f32x16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        const int row = row0 + (lane & 31), hh = lane >> 5;
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) {
+            const float4 a = *reinterpret_cast<const float4*>(ktile + TL::at(row, 16 * (2 * c + hh)));
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, q[c].x, s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, q[c].y, s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, q[c].z, s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, q[c].w, s, 0, 0, 0);
+        }
+        return s;
+    }
+    static __device__ __forceinline__ void add_values(const char* vtile, int row0, const f32x16& p, f32x16 (&o)[D / 32],
+                                                      int lane) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int row = row0 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db) {
+                const float a = *reinterpret_cast<const float*>(vtile + TL::at(row, 4 * (32 * db + (lane & 31))));
+                o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[i], o[db], 0, 0, 0);
+            }
+        }
+    }
+};
+
+// The elements of a word as a pass takes them: pass 1 finite ones (others 0),
+// passes 2, 3, 4 ones in place of +infinity, -infinity, NaN (others 0).
+template <typename T>
+__device__ __forceinline__ uint32_t only_special(uint32_t w, int pass) {
+    auto of = [&](uint32_t bits) {  // fp32
+        const bool special = (bits & 0x7f800000u) == 0x7f800000u, nan = (bits & 0x7fffffu) != 0;
+        if (pass == 1) return special ? 0u : bits;
+        const bool on = special && (pass == 4 ? nan : !nan && (bits >> 31) == (pass == 3));
+        return on ? 0x3f800000u : 0u;
+    };
+    if constexpr (sizeof(T) == 4) return of(w);
+    return (of(w << 16) >> 16) | of(w & 0xffff0000u);
+}
+
+// Shape of a workgroup: WR x 32 rows, tiles of BK keys of which each of the WK
+// groups of waves takes KS x 32.
+template <typename T, int D, int WR, int WK>
+struct Shape {
+    static constexpr int NW = WR * WK;
+    static constexpr int KS = (sizeof(T) == 2 && WK == 1) ? 2 : 1;
+    static constexpr int BK = 32 * WK * KS;
+    static constexpr int BM = 32 * WR;
+    static constexpr int kTile = BK * Tile<T, D>::RB;      // bytes of one K or V tile
+    static constexpr int kState = 32 * (D + 4) * 4;        // bytes of one wave's state (WK > 1)
+    static constexpr int kBuf = 2 * kTile > (WK > 1 ? NW * kState / 2 : 0) ? 2 * kTile : NW * kState / 2;
+    static_assert(kTile % (1024 * NW) == 0, "a tile is a whole number of 1 KB copies per wave");
+};
+
+// Attention of one block of rows over tiles of a stretch of keys.
+//   rowinfo(r)   RowInfo of the block's row r < BM
+//   qrow(r)      its query row (only of valid rows)
+//   docs         (EXTRA only) document of each key, or null; ranges: lowest and highest of
+//                every kDocTile keys
+//   split/splits the part of the block's key tiles to walk
+//   emit(r, dim, o, m, l)  receives four unnormalised values of row r
+// buf0, buf1: Shape::kBuf bytes of LDS each.
+template <typename T, int D, int NT, int WR, int WK, bool EXTRA, bool EXACT, typename Info, typename QRow, typename Emit>
+__device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, const int* docs, const int2* ranges,
+                                       int split, int splits, char* buf0, char* buf1, Info&& rowinfo, QRow&& qrow,
+                                       Emit&& emit) {
+    using SH = Shape<T, D, WR, WK>;
+    using TL = Tile<T, D>;
+    using OP = Ops<T, D, NT>;
+    constexpr int BK = SH::BK, KS = SH::KS, NW = SH::NW;
+    const int lane = lane_id(), hh = lane >> 5;
+    const int wv = __builtin_amdgcn_readfirstlane(wave_id());
+    const int wr = wv % WR, wk = wv / WR;
+
+    // keys that any row of the block may attend, and its rows' documents
+    int blo = seg.n, bhi = 0, dlo = 0x7fffffff, dhi = -0x7fffffff - 1;
+#pragma unroll
+    for (int r = lane; r < SH::BM; r += kWave) {
+        const RowInfo x = rowinfo(r);
+        if (x.valid && x.lo < x.hi) {
+            blo = min(blo, x.lo);
+            bhi = max(bhi, x.hi);
+        }
+        if (x.valid) {
+            dlo = min(dlo, x.doc);
+            dhi = max(dhi, x.doc);
+        }
+    }
+    blo = wave_min_i32(blo);
+    bhi = wave_max_i32(bhi);
+    if (EXTRA && docs) {
+        dlo = wave_min_i32(dlo);
+        dhi = wave_max_i32(dhi);
+    }
+    const RowInfo me = rowinfo(32 * wr + (lane & 31));
+    // keys that every row of the wave may attend, and that any may
+    const int wlo = wave_max_i32(me.valid ? me.lo : 0), whi = wave_min_i32(me.valid ? me.hi : seg.n);
+    const int vlo = wave_min_i32(me.valid ? me.lo : seg.n), vhi = wave_max_i32(me.valid ? me.hi : 0);
+
+    // this split's tiles
+    int t0 = blo / BK, t1 = bhi > blo ? (bhi + BK - 1) / BK : t0;
+    {
+        const int n = t1 - t0, per = (n + splits - 1) / splits;
+        t0 += min(n, split * per);
+        t1 = min(t1, t0 + per);
+    }
+
+    // the next tile from t on whose keys share a document with the block
+    auto next = [&](int t) {
+        if (EXTRA && docs) {
+            constexpr int RT = BK / kDocTile;
+            const int nr = (seg.n + kDocTile - 1) / kDocTile;
+            while (t < t1) {
+                bool on = false;
+                if (t + lane < t1) {
+#pragma unroll
+                    for (int k = 0; k < RT; ++k) {
+                        const int i = (t + lane) * RT + k;
+                        if (i < nr) {
+                            const int2 x = ranges[i];
+                            on = on || (x.y >= 0 && x.x <= dhi && x.y >= dlo);
+                        }
+                    }
+                }
+                const uint64_t any = __ballot(on);
+                if (any) return min(t1, t + __builtin_ctzll(any));
+                t += kWave;
+            }
+            return t1;
+        }
+        return t;
+    };
+    // A wave's 1 KB copies take every NW-th group of rows: row0 + step i, whose
+    // permutation differs from row0's by that of step i.
+    constexpr int RPC = 64 / TL::SPR, STEP = NW * RPC;
+    const int row0 = wv * RPC + lane / TL::SPR;
+    const uint32_t piece0 = 16 * ((lane % TL::SPR) ^ TL::perm(row0));
+    const uint32_t koff = static_cast<uint32_t>(row0 * seg.kt), voff = static_cast<uint32_t>(row0 * seg.vt);
+    auto copy = [&](int t, char* buf) {
+        constexpr int N = SH::kTile / (1024 * NW);  // copies per wave
+        static_assert((STEP & (STEP - 1)) == 0 && N * STEP == BK, "whole groups");
+        char* to = buf + 1024 * wv;
+        const char* kb = seg.K + static_cast<long long>(t) * BK * seg.kt;
+        const char* vb = seg.V + static_cast<long long>(t) * BK * seg.vt;
+        auto both = [&](int i, const char* k, const char* v, auto ko, auto vo) {
+            const uint32_t piece = piece0 ^ (16 * TL::perm(STEP * i));
+            __builtin_amdgcn_global_load_lds(
+                k + (ko + piece), (__attribute__((address_space(3))) void*)(to + 1024 * NW * i), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds(
+                v + (vo + piece), (__attribute__((address_space(3))) void*)(to + SH::kTile + 1024 * NW * i), 16, 0, 0);
+        };
+        const int last = seg.n - 1 - t * BK;
+        if (last >= BK - 1) {  // uniform
+            const long long ks = STEP * seg.kt, vs = STEP * seg.vt;
+#pragma unroll
+            for (int i = 0; i < N; ++i, kb += ks, vb += vs) both(i, kb, vb, koff, voff);
+        } else {  // rows behind the last key repeat it
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int r = min(row0 + STEP * i, last);
+                both(i, kb, vb, r * seg.kt, r * seg.vt);
+            }
+        }
+    };
+
+    OP op;
+    op.load_q(qrow(me.valid ? 32 * wr + (lane & 31) : 0), hh);
+    float m, l;
+    f32x16 o[D / 32];
+
+    // Pass 0 is the attention.  Where V holds a NaN or an infinity, the product
+    // carries it into every row of the block, also those that mask its key
+    // (0 times infinity).  A block that finds a value that is not finite in its
+    // sums therefore walks its tiles four times more: over V's +infinities,
+    // -infinities and NaNs as ones, with ones for the weights of unmasked keys,
+    // which says where they belong (has[]), and over V with zeros in their place.
+    int pass = 0;
+    auto compute = [&](int t, const char* buf, auto special) {
+        constexpr bool SPECIAL = decltype(special)::value;
+        const int k0 = t * BK + wk * 32 * KS;  // the wave's first key of the tile
+        if (k0 >= vhi || k0 + 32 * KS <= vlo) return;
+        f32x16 s[KS];
+#pragma unroll
+        for (int u = 0; u < KS; ++u) s[u] = op.scores(buf, wk * 32 * KS + 32 * u, lane);
+        if constexpr (EXTRA) {
+            if (sc.capped) {
+#pragma unroll
+                for (int u = 0; u < KS; ++u)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[u][i] = sc.cap_log2 * tanh_of<EXACT>(s[u][i] * sc.inv_cap);
+            } else {
+#pragma unroll
+                for (int u = 0; u < KS; ++u)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[u][i] *= sc.scale_log2;
+            }
+            if (sc.slopes) {
+            const float far = static_cast<float>(me.pos - k0 - 4 * hh);
+#pragma unroll
+            for (int u = 0; u < KS; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    s[u][i] = fmaf(-me.slope, fabsf(far - static_cast<float>(32 * u + 8 * (i / 4) + i % 4)), s[u][i]);
+            }
+        }
+        const bool masked = k0 < wlo || k0 + 32 * KS > whi;
+        if (masked) {
+#pragma unroll
+            for (int u = 0; u < KS; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int j = k0 + 32 * u + 8 * (i / 4) + 4 * hh + i % 4;
+                    if (j < me.lo || j >= me.hi) s[u][i] = kNegInf;
+                }
+        }
+        if (EXTRA && docs) {
+#pragma unroll
+            for (int u = 0; u < KS; ++u) {
+                const int2 x = ranges[min((k0 + 32 * u) / kDocTile, (seg.n - 1) / kDocTile)];
+                if (x.x == x.y && dlo == dhi && x.x == dlo && dlo >= 0) continue;  // one document
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int j = min(k0 + 32 * u + 8 * (i / 4) + 4 * hh + i % 4, seg.n - 1);
+                    if (docs[j] != me.doc || me.doc < 0) s[u][i] = kNegInf;
+                }
+            }
+        }
+        uint32_t open[KS];  // keys not masked (pass > 1)
+        if (SPECIAL && pass > 1) {
+#pragma unroll
+            for (int u = 0; u < KS; ++u) {
+                open[u] = 0;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) open[u] |= s[u][i] == kNegInf ? 0u : 1u << i;
+            }
+        }
+        float top = kNegInf;
+#pragma unroll
+        for (int u = 0; u < KS; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
+        top = fmaxf(top, other_half(top));
+        if constexpr (!EXTRA) top *= sc.scale_log2;
+        // the reference m moves only where a score exceeds it by more than 8
+        // (weights up to 2^8 are as exact as those below 1)
+        if (__any(top > m + 8.f)) {
+            const float mn = fmaxf(m, top);
+            const float f = mn == kNegInf || (SPECIAL && pass > 1) ? 1.f : exp2_fast(m - mn);
+            l *= f;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[db][i] *= f;
+            m = mn;
+        }
+        const float ref = m == kNegInf ? 0.f : m;
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < KS; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[u][i] = exp2_fast(EXTRA ? s[u][i] - ref : fmaf(s[u][i], sc.scale_log2, -ref));
+                sum += s[u][i];
+            }
+        l += sum;
+        if (SPECIAL && pass > 1) {
+#pragma unroll
+            for (int u = 0; u < KS; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[u][i] = (open[u] >> i) & 1 ? 1.f : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < KS; ++u)
+            OP::add_values(buf + SH::kTile, wk * 32 * KS + 32 * u, s[u], o, lane);
+    };
+
+    // every wave's copies of a tile are in LDS before any wave reads it
+    auto arrived = [&]() {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+    // V as the pass takes it
+    auto prepare = [&](char* buf) {
+        for (int x = threadIdx.x; x < SH::kTile / 16; x += NW * kWave) {
+            uint32_t* p = reinterpret_cast<uint32_t*>(buf + SH::kTile + 16 * x);
+            for (int e = 0; e < 4; ++e) p[e] = only_special<T>(p[e], pass);
+        }
+        __syncthreads();
+    };
+    auto step = [&](int t, char* buf, auto special) {
+        if constexpr (decltype(special)::value) prepare(buf);
+        compute(t, buf, special);
+    };
+    // one tile ahead; the two buffers are distinct objects, so that the copies
+    // into one are known not to touch the reads of the other
+    const int first = next(t0);
+    auto walk = [&](auto special) {
+        int t = first;
+        m = kNegInf;
+        l = 0.f;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+        if (t >= t1) return;
+        copy(t, buf0);
+        for (;;) {
+            int n = next(t + 1);
+            arrived();
+            if (n < t1) copy(n, buf1);
+            step(t, buf0, special);
+            if (n >= t1) break;
+            t = n;
+            n = next(t + 1);
+            arrived();
+            if (n < t1) copy(n, buf0);
+            step(t, buf1, special);
+            if (n >= t1) break;
+            t = n;
+        }
+    };
+    walk(std::false_type{});
+    float z = 0.f;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z = fmaf(o[db][i], 0.f, z);
+    if (__syncthreads_or(me.valid && z != 0.f)) {
+        uint32_t has[3][D / 64];  // +infinity, -infinity, NaN of value 16 db + i
+#pragma unroll 1
+        for (pass = 4; pass > 0; --pass) {
+            walk(std::true_type{});
+            __syncthreads();  // the tiles are read before they are copied again
+#pragma unroll
+            for (int k = 2; k < 5; ++k) {
+                if (k != pass) continue;
+#pragma unroll
+                for (int w = 0; w < D / 64; ++w) {
+                    uint32_t bits = 0;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) bits |= o[2 * w + i / 16][i % 16] != 0.f ? 1u << i : 0u;
+                    has[k - 2][w] = bits;
+                }
+            }
+        }
+#pragma unroll
+        for (int w = 0; w < D / 64; ++w)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const uint32_t bit = 1u << i;
+                float x = o[2 * w + i / 16][i % 16];
+                if (has[0][w] & bit) x = __builtin_inff();
+                if (has[1][w] & bit) x = kNegInf;
+                if ((has[2][w] | (has[0][w] & has[1][w])) & bit) x = __builtin_nanf("");
+                o[2 * w + i / 16][i % 16] = x;
+            }
+    }
+    l += other_half(l);
+
+    if constexpr (WK == 1) {
+        if (me.valid) {
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    emit(32 * wr + (lane & 31), 32 * db + 2 * i + 4 * hh,
+                         make_float4(o[db][i], o[db][i + 1], o[db][i + 2], o[db][i + 3]), m, l);
+        }
+    } else {
+        // the WK states of a row meet in LDS
+        constexpr int ST = D + 4;
+        __syncthreads();
+        auto state = [&](int w) {
+            constexpr int HALF = (NW + 1) / 2;
+            return reinterpret_cast<float*>((w < HALF ? buf0 : buf1) + (w < HALF ? w : w - HALF) * SH::kState);
+        };
+        float* mine = state(wv) + (lane & 31) * ST;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<float4*>(mine + 32 * db + 2 * i + 4 * hh) =
+                    make_float4(o[db][i], o[db][i + 1], o[db][i + 2], o[db][i + 3]);
+        if (hh == 0) {
+            mine[D] = m;
+            mine[D + 1] = l;
+        }
+        __syncthreads();
+        for (int x = threadIdx.x; x < SH::BM * (D / 4); x += NW * kWave) {
+            const int r = x / (D / 4), dim = 4 * (x % (D / 4));
+            if (!rowinfo(r).valid) continue;
+            float mm = kNegInf;
+#pragma unroll
+            for (int k = 0; k < WK; ++k) mm = fmaxf(mm, state(k * WR + r / 32)[(r % 32) * ST + D]);
+            float ll = 0.f;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < WK; ++k) {
+                const float* p = state(k * WR + r / 32) + (r % 32) * ST;
+                const float f = p[D] == kNegInf ? 0.f : exp2_fast(p[D] - mm);
+                const float4 y = *reinterpret_cast<const float4*>(p + dim);
+                ll += f * p[D + 1];
+                v.x += f * y.x;
+                v.y += f * y.y;
+                v.z += f * y.z;
+                v.w += f * y.w;
+            }
+            emit(r, dim, v, mm, ll);
+        }
+    }
+}
+
+__device__ __forceinline__ void store4(float* p, float4 v, float f) {
+    *reinterpret_cast<float4*>(p) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+}
+__device__ __forceinline__ void store4(bf16_t* p, float4 v, float f) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    bf16x4 b;
+    b[0] = static_cast<__bf16>(v.x * f);
+    b[1] = static_cast<__bf16>(v.y * f);
+    b[2] = static_cast<__bf16>(v.z * f);
+    b[3] = static_cast<__bf16>(v.w * f);
+    *reinterpret_cast<bf16x4*>(p) = b;
+}
+
+// 1 / l, 0 for a row that attended nothing.
+__device__ __forceinline__ float inverse_sum(float l) { return l == 0.f ? 0.f : 1.f / l; }
+
+__device__ __forceinline__ int clamp_pos(long long x) {
+    constexpr long long most = 1 << 30;
+    return static_cast<int>(x < -most ? -most : x > most ? most : x);
+}
+
+}  // namespace santapp

@@ -1,0 +1,205 @@
+// Decoding of several sequences over a prompt they share: each prompt's keys and
+// values are read once for all its sequences, each sequence's suffix rows once
+// for its heads, and the parts are joined.
+#include "attention_kernels.h"
+
+namespace santapp {
+
+namespace {
+
+__device__ __forceinline__ int clamped(const int* p, int i, int most) {
+    return p ? min(max(p[i], 0), most) : most;
+}
+
+template <typename T, int D, int WR, int WK, bool EXTRA>
+__global__ __launch_bounds__(64 * WR * WK) void k_prefix(PrefixArgs a) {
+    constexpr bool f32 = sizeof(T) == 4;
+    constexpr int NT = f32 ? 1 : 3;  // bf16 terms of a query
+    constexpr int SK = WR * WK;      // the suffix: all waves over keys, one block of rows
+    using SH = Shape<T, D, WR, WK>;
+    constexpr int kSuffix = WR == 1 ? WK : (f32 ? 2 : SK);
+    using SS = Shape<T, D, SK / kSuffix, kSuffix>;
+    constexpr int kBuf = SH::kBuf > SS::kBuf ? SH::kBuf : SS::kBuf;
+    __shared__ __align__(16) char buf0[kBuf];
+    __shared__ __align__(16) char buf1[kBuf];
+    const int Hq = a.Hkv * a.G;
+    const int prompts = a.P * a.Hkv * a.row_blocks * a.part.splits;
+    int x = blockIdx.x;
+    if (x < prompts) {
+        const int pairs = a.P * a.Hkv, R = a.S * a.G;
+        const int pair = x % pairs;
+        x /= pairs;
+        const int split = x % a.part.splits, r0 = x / a.part.splits * SH::BM;
+        const int p = pair / a.Hkv, kv = pair - p * a.Hkv;
+        KeySeg seg;
+        seg.K = a.K.p + p * a.K.b + kv * a.K.h;
+        seg.V = a.V.p + p * a.V.b + kv * a.V.h;
+        seg.kt = a.K.t;
+        seg.vt = a.V.t;
+        seg.n = clamped(a.prefix_lengths, p, a.N);
+        auto rowinfo = [&](int r) {
+            RowInfo x;
+            x.valid = r0 + r < R;
+            const int row = min(r0 + r, R - 1), i = row / a.G, b = p * a.S + i, h = kv * a.G + row - i * a.G;
+            const long long pos = a.positions ? static_cast<long long>(a.positions[b])
+                                              : static_cast<long long>(seg.n) + clamped(a.lengths, b, a.T) - 1;
+            x.pos = clamp_pos(pos);
+            x.lo = 0;
+            x.hi = seg.n;
+            if (a.score.window > 0) {
+                x.lo = static_cast<int>(min(max(pos - a.score.window + 1, 0ll), static_cast<long long>(seg.n)));
+                x.hi = static_cast<int>(min(max(pos + a.score.window, 0ll), static_cast<long long>(seg.n)));
+            }
+            x.doc = 0;
+            x.slope = EXTRA && a.score.slopes ? a.score.slopes[h] * 1.44269504088896341f : 0.f;
+            return x;
+        };
+        auto head = [&](int r) {
+            const int row = r0 + r, i = row / a.G;
+            return (static_cast<long long>(p) * a.S + i) * Hq + kv * a.G + row - i * a.G;
+        };
+        auto qrow = [&](int r) { return reinterpret_cast<const char*>(a.q + head(r) * D); };
+        auto emit = [&](int r, int dim, float4 v, float m, float l) {
+            if (a.part.splits + a.spart.splits > 1)
+                store_part<D>(a.part, pair, split, R, r0 + r, dim, v, m, l);
+            else
+                store4(a.out + head(r) * D + dim, v, inverse_sum(l));
+        };
+        attend<T, D, NT, WR, WK, EXTRA, true>(seg, a.score, nullptr, nullptr, split, a.part.splits, buf0, buf1, rowinfo, qrow,
+                                            emit);
+        return;
+    }
+    x -= prompts;
+    const int pairs = a.P * a.S * a.Hkv;
+    const int pair = x % pairs;
+    x /= pairs;
+    const int split = x % a.spart.splits, r0 = x / a.spart.splits * SS::BM;
+    const int b = pair / a.Hkv, kv = pair - b * a.Hkv, p = b / a.S;
+    KeySeg seg;
+    seg.K = a.sK.p + b * a.sK.b + kv * a.sK.h;
+    seg.V = a.sV.p + b * a.sV.b + kv * a.sV.h;
+    seg.kt = a.sK.t;
+    seg.vt = a.sV.t;
+    seg.n = clamped(a.lengths, b, a.T);
+    const long long pos = (a.positions ? static_cast<long long>(a.positions[b]) - clamped(a.prefix_lengths, p, a.N)
+                                       : static_cast<long long>(seg.n) - 1);
+    auto rowinfo = [&](int r) {
+        RowInfo x;
+        x.valid = r0 + r < a.G;
+        x.pos = clamp_pos(pos);
+        x.lo = 0;
+        x.hi = seg.n;
+        if (a.score.window > 0) {
+            x.lo = static_cast<int>(min(max(pos - a.score.window + 1, 0ll), static_cast<long long>(seg.n)));
+            x.hi = static_cast<int>(min(max(pos + a.score.window, 0ll), static_cast<long long>(seg.n)));
+        }
+        x.doc = 0;
+        x.slope = EXTRA && a.score.slopes ? a.score.slopes[kv * a.G + min(r0 + r, a.G - 1)] * 1.44269504088896341f : 0.f;
+        return x;
+    };
+    auto head = [&](int r) { return static_cast<long long>(b) * Hq + kv * a.G + r0 + r; };
+    auto qrow = [&](int r) { return reinterpret_cast<const char*>(a.q + head(r) * D); };
+    auto emit = [&](int r, int dim, float4 v, float m, float l) {
+        if (a.part.splits + a.spart.splits > 1)
+            store_part<D>(a.spart, pair, split, a.G, r0 + r, dim, v, m, l);
+        else
+            store4(a.out + head(r) * D + dim, v, inverse_sum(l));
+    };
+    attend<T, D, NT, SK / kSuffix, kSuffix, EXTRA, true>(seg, a.score, nullptr, nullptr, split, a.spart.splits, buf0, buf1,
+                                                       rowinfo, qrow, emit);
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs a) {
+    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    const int Hq = a.Hkv * a.G;
+    const long long row = i / (D / 4), b = row / Hq;
+    if (b >= static_cast<long long>(a.P) * a.S) return;
+    const int dim = 4 * static_cast<int>(i % (D / 4)), h = static_cast<int>(row - b * Hq), kv = h / a.G, g = h - kv * a.G;
+    const long long p = b / a.S, R = static_cast<long long>(a.S) * a.G;
+    const long long f0 = (p * a.Hkv + kv) * a.part.splits * R + (b - p * a.S) * a.G + g;
+    const long long f1 = (b * a.Hkv + kv) * a.spart.splits * a.G + g;
+    const JoinRun runs[2] = {{a.part.ml + f0, a.part.o + f0 * D, R, a.part.splits},
+                             {a.spart.ml + f1, a.spart.o + f1 * D, a.G, a.spart.splits}};
+    float l;
+    const float4 v = join_parts<D>(runs, dim, l);
+    store4(a.out + row * D + dim, v, inverse_sum(l));
+}
+
+template <typename T, int D>
+hipError_t launch(const PrefixArgs& a, hipStream_t s) {
+    constexpr bool f32 = sizeof(T) == 4;
+    const long long n = static_cast<long long>(a.P) * a.Hkv * a.row_blocks * a.part.splits +
+                        static_cast<long long>(a.P) * a.S * a.Hkv * a.srow_blocks * a.spart.splits;
+    const dim3 grid(static_cast<unsigned>(n));
+    const bool extra = a.score.capped || a.score.slopes;
+#define SANTAPP_PREFIX(V)                                                                                      \
+    case V:                                                                                                    \
+        if (extra)                                                                                             \
+            k_prefix<T, D, row_waves(V), key_waves(V, f32), true>                                              \
+                <<<grid, 64 * row_waves(V) * key_waves(V, f32), 0, s>>>(a);                                    \
+        else                                                                                                   \
+            k_prefix<T, D, row_waves(V), key_waves(V, f32), false>                                             \
+                <<<grid, 64 * row_waves(V) * key_waves(V, f32), 0, s>>>(a);                                    \
+        break;
+    switch (a.variant) {
+        SANTAPP_PREFIX(0)
+        SANTAPP_PREFIX(1)
+        SANTAPP_PREFIX(2)
+    }
+#undef SANTAPP_PREFIX
+    if (hipError_t e = hipGetLastError()) return e;
+    if (a.part.splits + a.spart.splits > 1) {
+        const long long rows = static_cast<long long>(a.P) * a.S * a.Hkv * a.G * (D / 4);
+        k_prefix_join<D><<<dim3(static_cast<unsigned>((rows + 255) / 256)), 256, 0, s>>>(a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t plan_prefix(PrefixArgs& a, int cus, char* ws) {
+    if (cus <= 0) cus = 256;
+    const bool f32 = a.dtype == SANTAPP_FP32;
+    const long long R = static_cast<long long>(a.S) * a.G, pairs = static_cast<long long>(a.P) * a.Hkv;
+    a.variant = variant_of(R);
+    const int bm = 32 * row_waves(a.variant), bk = tile_keys(a.variant, f32);
+    a.row_blocks = a.N > 0 ? static_cast<int>((R + bm - 1) / bm) : 0;
+    const long long blocks = pairs * a.row_blocks;
+    long long splits = 0;
+    if (blocks > 0) {
+        const long long tiles = (a.N + bk - 1) / bk;
+        splits = (2 * cus + blocks - 1) / blocks;
+        if (splits > tiles / 2) splits = tiles / 2;
+        splits = splits < 1 ? 1 : splits > 256 ? 256 : splits;
+    }
+    a.part.splits = static_cast<int>(splits);
+    // the suffixes: their rows are one block of 32 x SK / kSuffix per 32 heads
+    const int waves = row_waves(a.variant) * key_waves(a.variant, f32);
+    const int kw = row_waves(a.variant) == 1 ? key_waves(a.variant, f32) : (f32 ? 2 : waves);
+    const int sbm = 32 * (waves / kw);
+    a.srow_blocks = a.T > 0 ? (a.G + sbm - 1) / sbm : 0;
+    a.spart.splits = 0;
+    if (a.T > 0) {
+        const long long sblocks = pairs * a.S * a.srow_blocks;
+        const long long tiles = (a.T + 32 * kw - 1) / (32 * kw);
+        long long k = cus / sblocks;
+        k = k > tiles / 2 ? tiles / 2 : k;
+        a.spart.splits = static_cast<int>(k < 1 ? 1 : k > 64 ? 64 : k);
+    }
+    if (a.part.splits + a.spart.splits <= 1) return 0;
+    size_t at = 0;
+    if (a.part.splits) at += place_parts(a.part, pairs, R, a.d, ws, at);
+    if (a.spart.splits) at += place_parts(a.spart, pairs * a.S, a.G, a.d, ws, at);
+    return at;
+}
+
+hipError_t launch_prefix(const PrefixArgs& a, hipStream_t s) {
+    if (a.part.splits + a.spart.splits == 0) {  // no rows at all: zeros
+        return launch_zero(a.out, static_cast<size_t>(a.P) * a.S * a.Hkv * a.G * a.d * sizeof(float), s);
+    }
+    if (a.dtype == SANTAPP_BF16) return a.d == 128 ? launch<bf16_t, 128>(a, s) : launch<bf16_t, 64>(a, s);
+    return a.d == 128 ? launch<float, 128>(a, s) : launch<float, 64>(a, s);
+}
+
+}  // namespace santapp

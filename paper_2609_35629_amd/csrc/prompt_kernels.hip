@@ -1,0 +1,166 @@
+// Attention of a prompt's query tokens over its keys: causal, prefix, document
+// and window masks, capped scores, a bias by distance.
+#include "attention_kernels.h"
+
+namespace santapp {
+
+namespace {
+
+// Lowest and highest document of every kDocTile keys of a row [N].
+__global__ __launch_bounds__(256) void k_doc_ranges(const int* docs, int B, int N, int2* ranges) {
+    const int nr = (N + kDocTile - 1) / kDocTile;
+    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    const long long row = i / kDocTile / nr;
+    if (row >= B) return;  // whole 32-lane halves
+    const int r = static_cast<int>(i / kDocTile - row * nr);
+    const int doc = docs[row * N + min(r * kDocTile + static_cast<int>(i % kDocTile), N - 1)];
+    int lo = doc, hi = doc;
+#pragma unroll
+    for (int k = 1; k < kDocTile; k *= 2) {
+        lo = min(lo, __shfl_xor(lo, k));
+        hi = max(hi, __shfl_xor(hi, k));
+    }
+    if (i % kDocTile == 0) ranges[row * nr + r] = make_int2(lo, hi);
+}
+
+template <typename T, int D, int WR, int WK, bool EXTRA>
+__global__ __launch_bounds__(64 * WR * WK) void k_prompt(PromptArgs a) {
+    using SH = Shape<T, D, WR, WK>;
+    __shared__ __align__(16) char buf0[SH::kBuf];
+    __shared__ __align__(16) char buf1[SH::kBuf];
+    const int BH = a.B * a.Hkv, R = a.T * a.G;
+    // pairs fastest, so that a pair's blocks share an XCD's cache where the
+    // pairs divide the XCDs; the last rows (under a causal mask the longest) first
+    int x = blockIdx.x;
+    const int pair = x % BH;
+    x /= BH;
+    const int split = x % a.part.splits;
+    const int block = a.row_blocks - 1 - x / a.part.splits;
+    const int b = pair / a.Hkv, kv = pair - b * a.Hkv, r0 = block * SH::BM;
+    KeySeg seg;
+    seg.K = a.K.p + b * a.K.b + kv * a.K.h;
+    seg.V = a.V.p + b * a.V.b + kv * a.V.h;
+    seg.kt = a.K.t;
+    seg.vt = a.V.t;
+    seg.n = a.N;
+    const int* docs = EXTRA && a.documents ? a.documents + static_cast<long long>(b) * a.N : nullptr;
+    const int prefix = a.prefix ? a.prefix[b] : 0;
+    auto rowinfo = [&](int r) {
+        RowInfo x;
+        x.valid = r0 + r < R;
+        const int row = min(r0 + r, R - 1), t = row / a.G, h = kv * a.G + row - t * a.G;
+        x.pos = a.offset + t;
+        int lo = 0, hi = a.N;
+        if (a.causal) hi = min(hi, max(x.pos + 1, prefix));
+        if (a.score.window > 0) {
+            lo = static_cast<int>(max(0ll, static_cast<long long>(x.pos) - a.score.window + 1));
+            hi = static_cast<int>(min(static_cast<long long>(hi), static_cast<long long>(x.pos) + a.score.window));
+        }
+        x.lo = lo;
+        x.hi = hi;
+        x.doc = docs ? docs[x.pos] : 0;
+        x.slope = EXTRA && a.score.slopes ? a.score.slopes[h] * 1.44269504088896341f : 0.f;
+        return x;
+    };
+    auto qrow = [&](int r) {
+        const int row = r0 + r, t = row / a.G, h = kv * a.G + row - t * a.G;
+        return a.q.p + b * a.q.b + h * a.q.h + t * a.q.t;
+    };
+    auto emit = [&](int r, int dim, float4 v, float m, float l) {
+        if (a.part.splits > 1) {
+            store_part<D>(a.part, pair, split, R, r0 + r, dim, v, m, l);
+            return;
+        }
+        const int row = r0 + r, t = row / a.G, h = kv * a.G + row - t * a.G;
+        char* p = const_cast<char*>(a.out.p) + b * a.out.b + h * a.out.h + t * a.out.t;
+        store4(reinterpret_cast<T*>(p) + dim, v, inverse_sum(l));
+    };
+    const int2* ranges = docs ? a.doc_range + static_cast<long long>(b) * ((a.N + kDocTile - 1) / kDocTile) : nullptr;
+    attend<T, D, 1, WR, WK, EXTRA, sizeof(T) == 4>(seg, a.score, docs, ranges, split, a.part.splits, buf0, buf1, rowinfo,
+                                                 qrow, emit);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_prompt_join(PromptArgs a) {
+    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    const long long R = static_cast<long long>(a.T) * a.G;
+    const long long row = i / (D / 4), pair = row / R;
+    if (pair >= static_cast<long long>(a.B) * a.Hkv) return;
+    const int dim = 4 * static_cast<int>(i % (D / 4)), r = static_cast<int>(row - pair * R);
+    const long long first = pair * a.part.splits * R + r;
+    const JoinRun runs[2] = {{a.part.ml + first, a.part.o + first * D, R, a.part.splits}, {nullptr, nullptr, 0, 0}};
+    float l;
+    const float4 v = join_parts<D>(runs, dim, l);
+    const int b = static_cast<int>(pair / a.Hkv), kv = static_cast<int>(pair - static_cast<long long>(b) * a.Hkv);
+    const int t = r / a.G, h = kv * a.G + r - t * a.G;
+    char* p = const_cast<char*>(a.out.p) + b * a.out.b + h * a.out.h + t * a.out.t;
+    store4(reinterpret_cast<T*>(p) + dim, v, inverse_sum(l));
+}
+
+template <typename T, int D>
+hipError_t launch(const PromptArgs& a, hipStream_t s) {
+    constexpr bool f32 = sizeof(T) == 4;
+    const long long BH = static_cast<long long>(a.B) * a.Hkv, R = static_cast<long long>(a.T) * a.G;
+    if (a.documents && a.N > 0) {
+        const long long n = static_cast<long long>(a.B) * ((a.N + kDocTile - 1) / kDocTile) * kDocTile;
+        k_doc_ranges<<<dim3(static_cast<unsigned>((n + 255) / 256)), 256, 0, s>>>(a.documents, a.B, a.N, a.doc_range);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    const dim3 grid(static_cast<unsigned>(BH * a.part.splits * a.row_blocks));
+    const bool extra = a.score.capped || a.score.slopes || a.documents;
+#define SANTAPP_PROMPT(V)                                                                                      \
+    case V:                                                                                                    \
+        if (extra)                                                                                             \
+            k_prompt<T, D, row_waves(V), key_waves(V, f32), true>                                              \
+                <<<grid, 64 * row_waves(V) * key_waves(V, f32), 0, s>>>(a);                                    \
+        else                                                                                                   \
+            k_prompt<T, D, row_waves(V), key_waves(V, f32), false>                                             \
+                <<<grid, 64 * row_waves(V) * key_waves(V, f32), 0, s>>>(a);                                    \
+        break;
+    switch (a.variant) {
+        SANTAPP_PROMPT(0)
+        SANTAPP_PROMPT(1)
+        SANTAPP_PROMPT(2)
+    }
+#undef SANTAPP_PROMPT
+    if (hipError_t e = hipGetLastError()) return e;
+    if (a.part.splits > 1) {
+        const long long n = BH * R * (D / 4);
+        k_prompt_join<T, D><<<dim3(static_cast<unsigned>((n + 255) / 256)), 256, 0, s>>>(a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t plan_prompt(PromptArgs& a, int cus, char* ws) {
+    if (cus <= 0) cus = 256;
+    const bool f32 = a.dtype == SANTAPP_FP32;
+    const long long R = static_cast<long long>(a.T) * a.G, BH = static_cast<long long>(a.B) * a.Hkv;
+    a.variant = variant_of(R);
+    const int bm = 32 * row_waves(a.variant), bk = tile_keys(a.variant, f32);
+    a.row_blocks = static_cast<int>((R + bm - 1) / bm);
+    // few blocks of rows: their keys are split until two workgroups per compute
+    // unit have work, two tiles each at least
+    const long long blocks = BH * a.row_blocks;
+    long long keys = a.N;
+    if (a.score.window > 0) keys = keys < 2ll * a.score.window + a.T ? keys : 2ll * a.score.window + a.T;
+    const long long tiles = (keys + bk - 1) / bk;
+    long long splits = blocks >= cus ? 1 : (2 * cus + blocks - 1) / blocks;
+    if (splits > tiles / 2) splits = tiles / 2;
+    a.part.splits = static_cast<int>(splits < 1 ? 1 : splits > 128 ? 128 : splits);
+    size_t at = 0;
+    if (a.documents) {
+        a.doc_range = reinterpret_cast<int2*>(ws);
+        at = (static_cast<size_t>(a.B) * ((a.N + kDocTile - 1) / kDocTile) * sizeof(int2) + 255) & ~static_cast<size_t>(255);
+    }
+    if (a.part.splits > 1) at += place_parts(a.part, BH, R, a.d, ws, at);
+    return at;
+}
+
+hipError_t launch_prompt(const PromptArgs& a, hipStream_t s) {
+    if (a.dtype == SANTAPP_BF16) return a.d == 128 ? launch<bf16_t, 128>(a, s) : launch<bf16_t, 64>(a, s);
+    return a.d == 128 ? launch<float, 128>(a, s) : launch<float, 64>(a, s);
+}
+
+}  // namespace santapp
