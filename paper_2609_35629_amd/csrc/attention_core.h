@@ -240,7 +240,7 @@ __device__ __forceinline__ uint32_t only_special(uint32_t w, int pass) {
 
 // Shape of a workgroup: WR x 32 rows, tiles of BK keys of which each of the WK
 // groups of waves takes KS x 32.
-template <typename T, int D, int WR, int WK>
+template <typename T, int D, int NT, int WR, int WK>
 struct Shape {
     static constexpr int NW = WR * WK;
     static constexpr int KS = (sizeof(T) == 2 && WK == 1) ? 2 : 1;
@@ -249,6 +249,10 @@ struct Shape {
     static constexpr int kTile = BK * Tile<T, D>::RB;      // bytes of one K or V tile
     static constexpr int kState = 32 * (D + 4) * 4;        // bytes of one wave's state (WK > 1)
     static constexpr int kBuf = 2 * kTile > (WK > 1 ? NW * kState / 2 : 0) ? 2 * kTile : NW * kState / 2;
+    // workgroups per compute unit that the LDS holds, two at most: a wave of
+    // each per SIMD, one's softmax beside the other's products; one where the
+    // registers of a wave (query terms, sums, scores) would not fit half a SIMD's
+    static constexpr int kPerCu = 2 * (2 * kBuf + 1024) <= 160 * 1024 && (D == 64 || (sizeof(T) == 2 && NT == 1)) ? 2 : 1;
     static_assert(kTile % (1024 * NW) == 0, "a tile is a whole number of 1 KB copies per wave");
 };
 
@@ -264,7 +268,7 @@ template <typename T, int D, int NT, int WR, int WK, bool EXTRA, bool EXACT, typ
 __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, const int* docs, const int2* ranges,
                                        int split, int splits, char* buf0, char* buf1, Info&& rowinfo, QRow&& qrow,
                                        Emit&& emit) {
-    using SH = Shape<T, D, WR, WK>;
+    using SH = Shape<T, D, NT, WR, WK>;
     using TL = Tile<T, D>;
     using OP = Ops<T, D, NT>;
     constexpr int BK = SH::BK, KS = SH::KS, NW = SH::NW;
@@ -609,22 +613,6 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
         }
     }
 }
-
-__device__ __forceinline__ void store4(float* p, float4 v, float f) {
-    *reinterpret_cast<float4*>(p) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
-}
-__device__ __forceinline__ void store4(bf16_t* p, float4 v, float f) {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    bf16x4 b;
-    b[0] = static_cast<__bf16>(v.x * f);
-    b[1] = static_cast<__bf16>(v.y * f);
-    b[2] = static_cast<__bf16>(v.z * f);
-    b[3] = static_cast<__bf16>(v.w * f);
-    *reinterpret_cast<bf16x4*>(p) = b;
-}
-
-// 1 / l, 0 for a row that attended nothing.
-__device__ __forceinline__ float inverse_sum(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
 __device__ __forceinline__ int clamp_pos(long long x) {
     constexpr long long most = 1 << 30;

@@ -6,8 +6,13 @@
 
 namespace santapp {
 
-// Joins the split parts of every row.  D / 4 lanes per row, four dims each; the
-// parts of a row come in up to two runs (prompt, suffix).
+// Joins the split parts of one row, a workgroup per row: threads take a part's
+// maximum and sum each, then D / 4 lanes (four dims each) the values of every
+// kGroups-th part, several in flight.  The parts come in up to two runs
+// (prompt, suffix) of at most kMaxParts in all.
+constexpr int kJoinThreads = 256;
+constexpr int kMaxParts = 320;
+
 struct JoinRun {
     const float2* ml;  // part i: ml[i stride], values o[i stride d]
     const float* o;
@@ -15,26 +20,93 @@ struct JoinRun {
     int n;
 };
 
-template <int D>
-__device__ __forceinline__ float4 join_parts(const JoinRun (&runs)[2], int dim, float& l) {
-    float m = kNegInf;
-    for (int x = 0; x < 2; ++x)
-        for (int i = 0; i < runs[x].n; ++i) m = fmaxf(m, runs[x].ml[i * runs[x].stride].x);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+__device__ __forceinline__ void store4(float* p, float4 v, float f) {
+    *reinterpret_cast<float4*>(p) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+}
+__device__ __forceinline__ void store4(bf16_t* p, float4 v, float f) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    bf16x4 b;
+    b[0] = static_cast<__bf16>(v.x * f);
+    b[1] = static_cast<__bf16>(v.y * f);
+    b[2] = static_cast<__bf16>(v.z * f);
+    b[3] = static_cast<__bf16>(v.w * f);
+    *reinterpret_cast<bf16x4*>(p) = b;
+}
+
+// 1 / l, 0 for a row that attended nothing.
+__device__ __forceinline__ float inverse_sum(float l) { return l == 0.f ? 0.f : 1.f / l; }
+
+template <int D, typename TO>
+__device__ __forceinline__ void join_parts(const JoinRun (&runs)[2], TO* out) {
+    constexpr int L = D / 4, kGroups = kJoinThreads / L, kW = kJoinThreads / kWave;
+    constexpr int kEach = (kMaxParts + kJoinThreads - 1) / kJoinThreads;
+    __shared__ float s_w[kMaxParts];
+    __shared__ float s_red[2 * kW];
+    __shared__ float4 s_v[kGroups][L];
+    const int n = runs[0].n + runs[1].n;
+    auto of = [&](int i, const float*& o) {
+        const int x = i < runs[0].n ? 0 : 1;
+        const long long at = (i - (x ? runs[0].n : 0)) * runs[x].stride;
+        o = runs[x].o + at * D;
+        return runs[x].ml + at;
+    };
+    const float* unused;
+    float2 ml[kEach];
+    float m = kNegInf, l = 0.f;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int i = threadIdx.x + k * kJoinThreads;
+        ml[k] = i < n ? *of(i, unused) : make_float2(kNegInf, 0.f);
+        if (ml[k].y != 0.f) m = fmaxf(m, ml[k].x);
+    }
+    m = wave_max_f32(m);
+    if (lane_id() == 0) s_red[wave_id()] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kW; ++w) m = fmaxf(m, s_red[w]);
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int i = threadIdx.x + k * kJoinThreads;
+        const float f = ml[k].y == 0.f ? 0.f : exp2_fast(ml[k].x - m);  // nothing attended: 0
+        if (i < n) s_w[i] = f;
+        l += f == 0.f ? 0.f : f * ml[k].y;
+    }
+#pragma unroll
+    for (int k = 1; k < kWave; k *= 2) l += __shfl_xor(l, k);
+    if (lane_id() == 0) s_red[kW + wave_id()] = l;
+    __syncthreads();
     l = 0.f;
-    for (int x = 0; x < 2; ++x)
-        for (int i = 0; i < runs[x].n; ++i) {
-            const float2 ml = runs[x].ml[i * runs[x].stride];
-            if (ml.y == 0.f) continue;  // nothing attended
-            const float f = exp2_fast(ml.x - m);
-            const float4 y = *reinterpret_cast<const float4*>(runs[x].o + i * runs[x].stride * D + dim);
-            l += f * ml.y;
-            v.x += f * y.x;
-            v.y += f * y.y;
-            v.z += f * y.z;
-            v.w += f * y.w;
+#pragma unroll
+    for (int w = 0; w < kW; ++w) l += s_red[kW + w];
+    const int g = threadIdx.x / L, c = threadIdx.x % L;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int i = g; i < n; i += kGroups) {
+        const float* o;
+        of(i, o);
+        const float f = s_w[i];
+        const float4 y = reinterpret_cast<const float4*>(o)[c];
+        if (f != 0.f) {  // a part of no weight may hold anything
+            v.x = fmaf(f, y.x, v.x);
+            v.y = fmaf(f, y.y, v.y);
+            v.z = fmaf(f, y.z, v.z);
+            v.w = fmaf(f, y.w, v.w);
         }
-    return v;
+    }
+    s_v[g][c] = v;
+    __syncthreads();
+    if (threadIdx.x < L) {
+        v = s_v[0][c];
+#pragma unroll
+        for (int k = 1; k < kGroups; ++k) {
+            const float4 y = s_v[k][c];
+            v.x += y.x;
+            v.y += y.y;
+            v.z += y.z;
+            v.w += y.w;
+        }
+        store4(out + 4 * c, v, inverse_sum(l));
+    }
 }
 
 // One split's part of row r of a pair: values, and (by the lane of dim 0) its

@@ -11,17 +11,28 @@ __device__ __forceinline__ int clamped(const int* p, int i, int most) {
     return p ? min(max(p[i], 0), most) : most;
 }
 
+// A workgroup takes a block of a prompt's rows, or (split over keys by SK of its
+// waves) one of a sequence's heads over its suffix.
+constexpr int suffix_key_waves(int v, bool f32) { return v == 0 ? key_waves(0, f32) : 2; }
+
+template <typename T, int D, int WR, int WK>
+struct PrefixShape {
+    static constexpr int SK = suffix_key_waves(variant_of(32 * WR), sizeof(T) == 4);
+    static constexpr int NT = sizeof(T) == 4 ? 1 : 3;  // bf16 terms of a query
+    using Prompt = Shape<T, D, NT, WR, WK>;
+    using Suffix = Shape<T, D, NT, WR * WK / SK, SK>;
+    static constexpr int kBuf = Prompt::kBuf > Suffix::kBuf ? Prompt::kBuf : Suffix::kBuf;
+    static constexpr int kPerCu = Prompt::kPerCu < Suffix::kPerCu ? Prompt::kPerCu : Suffix::kPerCu;
+};
+
 template <typename T, int D, int WR, int WK, bool EXTRA>
-__global__ __launch_bounds__(64 * WR * WK) void k_prefix(PrefixArgs a) {
-    constexpr bool f32 = sizeof(T) == 4;
-    constexpr int NT = f32 ? 1 : 3;  // bf16 terms of a query
-    constexpr int SK = WR * WK;      // the suffix: all waves over keys, one block of rows
-    using SH = Shape<T, D, WR, WK>;
-    constexpr int kSuffix = WR == 1 ? WK : (f32 ? 2 : SK);
-    using SS = Shape<T, D, SK / kSuffix, kSuffix>;
-    constexpr int kBuf = SH::kBuf > SS::kBuf ? SH::kBuf : SS::kBuf;
-    __shared__ __align__(16) char buf0[kBuf];
-    __shared__ __align__(16) char buf1[kBuf];
+__global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) void k_prefix(PrefixArgs a) {
+    using PS = PrefixShape<T, D, WR, WK>;
+    using SH = typename PS::Prompt;
+    using SS = typename PS::Suffix;
+    constexpr int SK = PS::SK, NT = PS::NT;
+    __shared__ __align__(16) char buf0[PS::kBuf];
+    __shared__ __align__(16) char buf1[PS::kBuf];
     const int Hq = a.Hkv * a.G;
     const int prompts = a.P * a.Hkv * a.row_blocks * a.part.splits;
     int x = blockIdx.x;
@@ -105,25 +116,19 @@ __global__ __launch_bounds__(64 * WR * WK) void k_prefix(PrefixArgs a) {
         else
             store4(a.out + head(r) * D + dim, v, inverse_sum(l));
     };
-    attend<T, D, NT, SK / kSuffix, kSuffix, EXTRA, true>(seg, a.score, nullptr, nullptr, split, a.spart.splits, buf0, buf1,
+    attend<T, D, NT, WR * WK / SK, SK, EXTRA, true>(seg, a.score, nullptr, nullptr, split, a.spart.splits, buf0, buf1,
                                                        rowinfo, qrow, emit);
 }
 
 template <int D>
-__global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs a) {
-    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
-    const int Hq = a.Hkv * a.G;
-    const long long row = i / (D / 4), b = row / Hq;
-    if (b >= static_cast<long long>(a.P) * a.S) return;
-    const int dim = 4 * static_cast<int>(i % (D / 4)), h = static_cast<int>(row - b * Hq), kv = h / a.G, g = h - kv * a.G;
-    const long long p = b / a.S, R = static_cast<long long>(a.S) * a.G;
-    const long long f0 = (p * a.Hkv + kv) * a.part.splits * R + (b - p * a.S) * a.G + g;
-    const long long f1 = (b * a.Hkv + kv) * a.spart.splits * a.G + g;
+__global__ __launch_bounds__(kJoinThreads) void k_prefix_join(PrefixArgs a) {
+    const int Hq = a.Hkv * a.G, row = blockIdx.x, b = row / Hq, h = row - b * Hq, kv = h / a.G, g = h - kv * a.G;
+    const int p = b / a.S, R = a.S * a.G;
+    const long long f0 = (static_cast<long long>(p) * a.Hkv + kv) * a.part.splits * R + (b - p * a.S) * a.G + g;
+    const long long f1 = (static_cast<long long>(b) * a.Hkv + kv) * a.spart.splits * a.G + g;
     const JoinRun runs[2] = {{a.part.ml + f0, a.part.o + f0 * D, R, a.part.splits},
                              {a.spart.ml + f1, a.spart.o + f1 * D, a.G, a.spart.splits}};
-    float l;
-    const float4 v = join_parts<D>(runs, dim, l);
-    store4(a.out + row * D + dim, v, inverse_sum(l));
+    join_parts<D>(runs, a.out + static_cast<long long>(row) * D);
 }
 
 template <typename T, int D>
@@ -150,8 +155,7 @@ hipError_t launch(const PrefixArgs& a, hipStream_t s) {
 #undef SANTAPP_PREFIX
     if (hipError_t e = hipGetLastError()) return e;
     if (a.part.splits + a.spart.splits > 1) {
-        const long long rows = static_cast<long long>(a.P) * a.S * a.Hkv * a.G * (D / 4);
-        k_prefix_join<D><<<dim3(static_cast<unsigned>((rows + 255) / 256)), 256, 0, s>>>(a);
+        k_prefix_join<D><<<dim3(static_cast<unsigned>(a.P * a.S * a.Hkv * a.G)), kJoinThreads, 0, s>>>(a);
     }
     return hipGetLastError();
 }
@@ -174,10 +178,8 @@ size_t plan_prefix(PrefixArgs& a, int cus, char* ws) {
         splits = splits < 1 ? 1 : splits > 256 ? 256 : splits;
     }
     a.part.splits = static_cast<int>(splits);
-    // the suffixes: their rows are one block of 32 x SK / kSuffix per 32 heads
-    const int waves = row_waves(a.variant) * key_waves(a.variant, f32);
-    const int kw = row_waves(a.variant) == 1 ? key_waves(a.variant, f32) : (f32 ? 2 : waves);
-    const int sbm = 32 * (waves / kw);
+    const int kw = suffix_key_waves(a.variant, f32);
+    const int sbm = 32 * (row_waves(a.variant) * key_waves(a.variant, f32) / kw);
     a.srow_blocks = a.T > 0 ? (a.G + sbm - 1) / sbm : 0;
     a.spart.splits = 0;
     if (a.T > 0) {

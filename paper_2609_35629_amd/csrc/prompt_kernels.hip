@@ -24,8 +24,8 @@ __global__ __launch_bounds__(256) void k_doc_ranges(const int* docs, int B, int 
 }
 
 template <typename T, int D, int WR, int WK, bool EXTRA>
-__global__ __launch_bounds__(64 * WR * WK) void k_prompt(PromptArgs a) {
-    using SH = Shape<T, D, WR, WK>;
+__global__ __launch_bounds__(64 * WR * WK, (Shape<T, D, 1, WR, WK>::kPerCu)) void k_prompt(PromptArgs a) {
+    using SH = Shape<T, D, 1, WR, WK>;
     __shared__ __align__(16) char buf0[SH::kBuf];
     __shared__ __align__(16) char buf1[SH::kBuf];
     const int BH = a.B * a.Hkv, R = a.T * a.G;
@@ -81,20 +81,13 @@ __global__ __launch_bounds__(64 * WR * WK) void k_prompt(PromptArgs a) {
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void k_prompt_join(PromptArgs a) {
-    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
-    const long long R = static_cast<long long>(a.T) * a.G;
-    const long long row = i / (D / 4), pair = row / R;
-    if (pair >= static_cast<long long>(a.B) * a.Hkv) return;
-    const int dim = 4 * static_cast<int>(i % (D / 4)), r = static_cast<int>(row - pair * R);
-    const long long first = pair * a.part.splits * R + r;
+__global__ __launch_bounds__(kJoinThreads) void k_prompt_join(PromptArgs a) {
+    const int R = a.T * a.G, pair = blockIdx.x / R, r = blockIdx.x - pair * R;
+    const long long first = static_cast<long long>(pair) * a.part.splits * R + r;
     const JoinRun runs[2] = {{a.part.ml + first, a.part.o + first * D, R, a.part.splits}, {nullptr, nullptr, 0, 0}};
-    float l;
-    const float4 v = join_parts<D>(runs, dim, l);
-    const int b = static_cast<int>(pair / a.Hkv), kv = static_cast<int>(pair - static_cast<long long>(b) * a.Hkv);
-    const int t = r / a.G, h = kv * a.G + r - t * a.G;
+    const int b = pair / a.Hkv, kv = pair - b * a.Hkv, t = r / a.G, h = kv * a.G + r - t * a.G;
     char* p = const_cast<char*>(a.out.p) + b * a.out.b + h * a.out.h + t * a.out.t;
-    store4(reinterpret_cast<T*>(p) + dim, v, inverse_sum(l));
+    join_parts<D>(runs, reinterpret_cast<T*>(p));
 }
 
 template <typename T, int D>
@@ -125,8 +118,7 @@ hipError_t launch(const PromptArgs& a, hipStream_t s) {
 #undef SANTAPP_PROMPT
     if (hipError_t e = hipGetLastError()) return e;
     if (a.part.splits > 1) {
-        const long long n = BH * R * (D / 4);
-        k_prompt_join<T, D><<<dim3(static_cast<unsigned>((n + 255) / 256)), 256, 0, s>>>(a);
+        k_prompt_join<T, D><<<dim3(static_cast<unsigned>(BH * R)), kJoinThreads, 0, s>>>(a);
     }
     return hipGetLastError();
 }
