@@ -388,7 +388,9 @@ santapp_status santapp_routing_kl(const santapp_teams* teams, const float* q, in
  * Rows of a tensor [B][heads][tokens] of d contiguous elements each: the first
  * row's address (16-byte aligned) and the distances between rows in elements
  * (not negative; of a dimension of more than one entry, a multiple of 16 bytes).
- * Inputs may repeat rows (distance 0), outputs may not share any.
+ * Inputs may repeat rows (distance 0), outputs may not share any, and the memory
+ * from an output's first to its last row may not meet an input's (EINVAL) but
+ * where a call says so.
  */
 typedef struct {
     void* data;

@@ -14,7 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import math
-from typing import Optional, Tuple, Union
+from typing import Optional, Union
 
 import torch
 
@@ -34,86 +34,80 @@ def _code(t: torch.Tensor, name: str) -> int:
     raise SantappError(_lib.EDTYPE, f"unsupported dtype {t.dtype} of {name}")
 
 
-def _rows(t: torch.Tensor, name: str, shape, device) -> _lib.Rows:
-    """The view ``t`` [B, H, T, d] as the library takes it."""
+def _on(t: torch.Tensor, name: str, stream):
+    """``(device, current device, stream handle)`` of a call over ``t``."""
+    if not t.is_cuda:
+        _fail(f"{name} must be a GPU tensor")
+    device = t.device
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    elif stream.device != device:
+        _fail(f"the stream is on {stream.device}, {name} on {device}")
+    return device, torch.cuda.current_device(), stream.cuda_stream
+
+
+def _call(device, current: int, function, *args) -> None:
+    """A library call with ``device`` as the current one."""
+    if device.index == current:
+        check(function(*args))
+    else:
+        with torch.cuda.device(device):
+            check(function(*args))
+
+
+def _misfit(t, name: str, shape, device, dtype=None):
+    """The error of a tensor that is not what a call needs."""
     if not t.is_cuda or t.device != device:
         _fail(f"{name} must be a GPU tensor on {device}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         _fail(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.numel() and t.stride(3) != 1:
-        _fail(f"{name}: rows must be contiguous")
-    return _lib.Rows(t.data_ptr(), *t.stride()[:3])
+    if dtype is not None and t.dtype != dtype:
+        _fail(f"{name} has dtype {t.dtype}, expected {dtype}")
+    _fail(f"{name}: rows must be contiguous" if dtype is None else f"{name} must be contiguous")
+
+
+def _rows(t: torch.Tensor, name: str, shape, device) -> _lib.Rows:
+    """The view ``t`` [B, H, T, d] as the library takes it."""
+    s = t.stride()
+    if t.device != device or t.shape != shape or (s[3] != 1 and t.numel()):
+        _misfit(t, name, shape, device)
+    return _lib.Rows(t.data_ptr(), s[0], s[1], s[2])
 
 
 def _array(t: Optional[torch.Tensor], name: str, shape, dtype, device):
     """Address of an optional dense array."""
     if t is None:
         return None
-    if not t.is_cuda or t.device != device:
-        _fail(f"{name} must be a GPU tensor on {device}")
-    if tuple(t.shape) != tuple(shape):
-        _fail(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.dtype != dtype:
-        _fail(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if not t.is_contiguous():
-        _fail(f"{name} must be contiguous")
-    return ctypes.c_void_p(t.data_ptr())
-
-
-class _On:
-    """The device of a call's tensors as the current one, and the stream."""
-
-    def __init__(self, t: torch.Tensor, name: str, stream):
-        if not t.is_cuda:
-            _fail(f"{name} must be a GPU tensor")
-        self.device = t.device
-        if stream is not None and stream.device != t.device:
-            _fail(f"the stream is on {stream.device}, {name} on {t.device}")
-        s = stream if stream is not None else torch.cuda.current_stream(t.device)
-        self.stream = ctypes.c_void_p(s.cuda_stream)
-        self._guard = torch.cuda.device(t.device)
-
-    def __enter__(self):
-        self._guard.__enter__()
-        return self
-
-    def __exit__(self, *e):
-        self._guard.__exit__(*e)
-        return False
+    if t.device != device or t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+        _misfit(t, name, shape, device, dtype)
+    return t.data_ptr()
 
 
 def _heads(t: torch.Tensor, name: str) -> torch.Tensor:
     """``[B, H, d]`` (one token) as ``[B, H, 1, d]``."""
-    if t.dim() == 3:
-        return t.unsqueeze(2)
-    if t.dim() != 4:
+    if t.dim() == 4:
+        return t
+    if t.dim() != 3:
         _fail(f"{name} must be [B, H, T, d] or [B, H, d]")
-    return t
+    return t.unsqueeze(2)
 
 
-def _same_memory(a: torch.Tensor, b: torch.Tensor) -> bool:
-    """Whether the address ranges of two tensors meet."""
-    if not a.numel() or not b.numel():
-        return False
-
-    def ends(t):
-        last = sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
-        return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
-    (a0, a1), (b0, b1) = ends(a), ends(b)
-    return a0 < b1 and b0 < a1
-
-
-def _scratch(workspace: Optional[torch.Tensor], need: int, device) -> Tuple[Optional[ctypes.c_void_p], int,
-                                                                           Optional[torch.Tensor]]:
+def _scratch(workspace: Optional[torch.Tensor], size, device, stream):
+    """Address and bytes of the caller's workspace, or of a new one of
+    ``size()`` bytes.  On a stream of the caller's, which need not be the
+    current one, a new one must not be given out again before that stream has
+    passed the call."""
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    elif not workspace.is_cuda or workspace.device != device:
-        _fail(f"workspace must be a GPU tensor on {device}")
-    elif not workspace.is_contiguous():
-        _fail("workspace must be contiguous")
-    if workspace is None:
-        return None, 0, None
-    return ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size(), workspace
+        need = size()
+        if not need:
+            return None, 0, None
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        if stream is not None:
+            workspace.record_stream(stream)
+        return workspace.data_ptr(), need, workspace
+    if workspace.device != device or not workspace.is_contiguous():
+        _misfit(workspace, "workspace", workspace.shape, device, workspace.dtype)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 # ---------------------------------------------------------------------------
@@ -157,8 +151,8 @@ def rope_frequencies(rot: int, base: float = 10000.0, scaling: Optional[str] = N
 
 
 def _rotation(freqs: torch.Tensor, interleaved: bool, magnitude: float, device) -> _lib.Rotation:
-    f = _array(freqs, "freqs", (freqs.numel(),), torch.float64, device)
-    return _lib.Rotation(f, freqs.numel(), int(bool(interleaved)), float(magnitude))
+    n = freqs.numel()
+    return _lib.Rotation(_array(freqs, "freqs", (n,), torch.float64, device), n, bool(interleaved), magnitude)
 
 
 def rope(x: torch.Tensor, freqs: torch.Tensor, positions: Optional[torch.Tensor] = None, first: int = 0,
@@ -169,26 +163,23 @@ def rope(x: torch.Tensor, freqs: torch.Tensor, positions: Optional[torch.Tensor]
     or (2 i, 2 i + 1) if ``interleaved``, by ``position * freqs[i]``, times
     ``magnitude``; the rest copied.  Token t is at ``positions [B, T]`` (int32;
     any value) or at ``first + t``.  ``out`` may be ``x`` itself."""
-    with _On(x, "x", stream) as on:
-        x4 = _heads(x, "x")
-        B, H, T, d = x4.shape
-        if out is None:
-            out = torch.empty_like(x4, dtype=out_dtype or x.dtype, memory_format=torch.contiguous_format).view(x.shape)
-        elif out_dtype is not None and out.dtype != out_dtype:
-            _fail(f"out has dtype {out.dtype}, expected {out_dtype}")
-        if out.shape != x.shape:
-            _fail(f"out has shape {tuple(out.shape)}, expected {tuple(x.shape)}")
-        o4 = _heads(out, "out")
-        if _same_memory(o4, x4) and not (o4.data_ptr() == x4.data_ptr() and o4.stride() == x4.stride() and
-                                         o4.dtype == x4.dtype):
-            _fail("out overlaps x without being x")
-        if positions is not None and positions.dim() == 1:
-            positions = positions.unsqueeze(1)
-        pos = _array(positions, "positions", (B, T), torch.int32, on.device)
-        r = _rotation(freqs, interleaved, magnitude, on.device)
-        xr, yr = _rows(x4, "x", (B, H, T, d), on.device), _rows(o4, "out", (B, H, T, d), on.device)
-        check(_lib.load().santapp_rope(ctypes.byref(r), ctypes.byref(xr), _code(x, "x"), B, H, T, d, pos, int(first),
-                                       ctypes.byref(yr), _code(out, "out"), on.stream))
+    device, current, s = _on(x, "x", stream)
+    x4 = _heads(x, "x")
+    if out is None:
+        out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=device)
+        if stream is not None:
+            out.record_stream(stream)
+    elif out_dtype is not None and out.dtype != out_dtype:
+        _fail(f"out has dtype {out.dtype}, expected {out_dtype}")
+    o4 = _heads(out, "out")
+    shape = x4.shape
+    B, H, T, d = shape
+    if positions is not None and positions.dim() == 1:
+        positions = positions.unsqueeze(1)
+    pos = _array(positions, "positions", (B, T), torch.int32, device)
+    r = _rotation(freqs, interleaved, magnitude, device)
+    _call(device, current, _lib.load().santapp_rope, r, _rows(x4, "x", shape, device), _code(x, "x"), B, H, T, d, pos,
+          first, _rows(o4, "out", shape, device), _code(out, "out"), s)
     return out
 
 
@@ -204,51 +195,41 @@ def rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cac
     (the caller advances it; rows outside the cache are dropped when it is a
     tensor, refused when it is a number).  Token t is at ``positions [B, T]`` or
     at ``first + at[b] + t``."""
-    with _On(k, "k", stream) as on:
-        k4, v4 = _heads(k, "k"), _heads(v, "v")
-        B, Hkv, T, d = k4.shape
-        if v.dtype != k.dtype or cache_V.dtype != cache_K.dtype:
-            _fail("k and v, and the two caches, must have one type each")
-        if cache_K.dim() != 4:
-            _fail("cache_K must be [B, Hkv, capacity, d]")
-        cap = cache_K.shape[2]
-        kr, vr = _rows(k4, "k", (B, Hkv, T, d), on.device), _rows(v4, "v", (B, Hkv, T, d), on.device)
-        ck = _rows(cache_K, "cache_K", (B, Hkv, cap, d), on.device)
-        cv = _rows(cache_V, "cache_V", (B, Hkv, cap, d), on.device)
-        Hq, qr, qo, qc, oc = 0, None, None, _lib.BF16, _lib.BF16
-        ins = [k4, v4]
-        outs = [cache_K, cache_V]
-        if q is not None:
-            q4 = _heads(q, "q")
-            Hq = q4.shape[1]
-            if q_out is None:
-                q_out = torch.empty(q.shape, dtype=torch.float32, device=on.device)
-            if q_out.shape != q.shape:
-                _fail(f"q_out has shape {tuple(q_out.shape)}, expected {tuple(q.shape)}")
-            o4 = _heads(q_out, "q_out")
-            qr = ctypes.byref(_rows(q4, "q", (B, Hq, T, d), on.device))
-            qo = ctypes.byref(_rows(o4, "q_out", (B, Hq, T, d), on.device))
-            qc, oc = _code(q, "q"), _code(q_out, "q_out")
-            if not (o4.data_ptr() == q4.data_ptr() and o4.stride() == q4.stride() and q.dtype == q_out.dtype):
-                ins.append(q4)
-            outs.append(o4)
-        elif q_out is not None:
-            _fail("q_out without q")
-        for i, o in enumerate(outs):
-            if any(_same_memory(o, x) for x in ins + outs[:i]):
-                _fail("the caches and q_out must not overlap the inputs or each other")
-        row0, rows = 0, None
-        if isinstance(at, torch.Tensor):
-            rows = _array(at, "at", (B,), torch.int32, on.device)
-        else:
-            row0 = int(at)
-        if positions is not None and positions.dim() == 1:
-            positions = positions.unsqueeze(1)
-        pos = _array(positions, "positions", (B, T), torch.int32, on.device)
-        r = _rotation(freqs, interleaved, magnitude, on.device)
-        check(_lib.load().santapp_rope_append(
-            ctypes.byref(r), qr, qc, qo, oc, ctypes.byref(kr), ctypes.byref(vr), _code(k, "k"), ctypes.byref(ck),
-            ctypes.byref(cv), _code(cache_K, "cache_K"), cap, B, Hq, Hkv, T, d, rows, row0, pos, int(first), on.stream))
+    device, current, s = _on(k, "k", stream)
+    k4, v4 = _heads(k, "k"), _heads(v, "v")
+    shape = k4.shape
+    B, Hkv, T, d = shape
+    if v.dtype != k.dtype or cache_V.dtype != cache_K.dtype:
+        _fail("k and v, and the two caches, must have one type each")
+    if cache_K.dim() != 4:
+        _fail("cache_K must be [B, Hkv, capacity, d]")
+    cap = cache_K.shape[2]
+    held = (B, Hkv, cap, d)
+    Hq, qr, qo, qc, oc = 0, None, None, 0, 0
+    if q is not None:
+        q4 = _heads(q, "q")
+        Hq = q4.shape[1]
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=torch.float32, device=device)
+            if stream is not None:
+                q_out.record_stream(stream)
+        qs = (B, Hq, T, d)
+        qr, qo = _rows(q4, "q", qs, device), _rows(_heads(q_out, "q_out"), "q_out", qs, device)
+        qc, oc = _code(q, "q"), _code(q_out, "q_out")
+    elif q_out is not None:
+        _fail("q_out without q")
+    row0, rows = 0, None
+    if isinstance(at, torch.Tensor):
+        rows = _array(at, "at", (B,), torch.int32, device)
+    else:
+        row0 = at
+    if positions is not None and positions.dim() == 1:
+        positions = positions.unsqueeze(1)
+    pos = _array(positions, "positions", (B, T), torch.int32, device)
+    _call(device, current, _lib.load().santapp_rope_append, _rotation(freqs, interleaved, magnitude, device), qr, qc, qo,
+          oc, _rows(k4, "k", shape, device), _rows(v4, "v", shape, device), _code(k, "k"),
+          _rows(cache_K, "cache_K", held, device), _rows(cache_V, "cache_V", held, device), _code(cache_K, "cache_K"), cap,
+          B, Hq, Hkv, T, d, rows, row0, pos, first, s)
     return q_out
 
 
@@ -258,23 +239,23 @@ def rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cac
 
 
 def _score(scale, softcap, slopes, window, Hq, device) -> _lib.Score:
-    return _lib.Score(float(scale), float(softcap), _array(slopes, "slopes", (Hq,), torch.float32, device), int(window))
+    return _lib.Score(scale, softcap, _array(slopes, "slopes", (Hq,), torch.float32, device), window)
 
 
 def prompt_workspace(B: int, Hq: int, Hkv: int, T: int, N: int, d: int, dtype: torch.dtype = torch.bfloat16,
                      window: int = 0, documents: bool = False, device="cuda") -> torch.Tensor:
     """Workspace of :func:`prompt_attention` at these sizes (uninitialised)."""
-    return torch.empty(max(_prompt_bytes(B, Hq, Hkv, T, N, d, dtype, window, documents, torch.device(device)), 1),
-                       dtype=torch.uint8, device=device)
-
-
-def _prompt_bytes(B, Hq, Hkv, T, N, d, dtype, window, documents, device) -> int:
     n = ctypes.c_size_t()
     with torch.cuda.device(device):
-        check(_lib.load().santapp_prompt_workspace_bytes(B, Hq, Hkv, T, N, d,
-                                                         _lib.BF16 if dtype == torch.bfloat16 else _lib.FP32,
-                                                         int(window), int(documents), ctypes.byref(n)))
-    return n.value
+        check(_lib.load().santapp_prompt_workspace_bytes(B, Hq, Hkv, T, N, d, _dtype(dtype), window, documents,
+                                                         ctypes.byref(n)))
+    return torch.empty(max(n.value, 1), dtype=torch.uint8, device=device)
+
+
+def _dtype(dtype: torch.dtype) -> int:
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise SantappError(_lib.EDTYPE, f"unsupported dtype {dtype}")
+    return _lib.BF16 if dtype == torch.bfloat16 else _lib.FP32
 
 
 def prompt_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, causal: bool = True,
@@ -291,69 +272,48 @@ def prompt_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, causal: 
     [B, N]`` (int32) are equal and not negative.  Scores are ``scale q.k`` (0:
     1 / sqrt(d)), capped by ``softcap * tanh(s / softcap)`` when ``softcap`` > 0, less
     ``slopes[h]`` per token of distance.  A query that attends nothing gets 0."""
-    with _On(q, "q", stream) as on:
-        if q.dim() != 4 or K.dim() != 4:
-            _fail("q and K must be [B, H, tokens, d]")
-        B, Hq, T, d = q.shape
-        Hkv, N = K.shape[1], K.shape[2]
-        if K.dtype != q.dtype or V.dtype != q.dtype:
-            _fail(f"q, K and V must have one type, got {q.dtype}, {K.dtype}, {V.dtype}")
-        code = _code(q, "q")
-        if offset is None:
-            offset = N - T if N >= T or causal else 0
-        if out is None:
-            out = torch.empty_like(q, memory_format=torch.preserve_format if _dense(q) else torch.contiguous_format)
-        if out.dtype != q.dtype:
-            _fail(f"out has dtype {out.dtype}, expected {q.dtype}")
-        if any(_same_memory(out, x) for x in (q, K, V)):
-            _fail("out must not overlap q, K or V")
-        qr, orr = _rows(q, "q", (B, Hq, T, d), on.device), _rows(out, "out", (B, Hq, T, d), on.device)
-        kr, vr = _rows(K, "K", (B, Hkv, N, d), on.device), _rows(V, "V", (B, Hkv, N, d), on.device)
-        sc = _score(scale, softcap, slopes, window, Hq, on.device)
-        docs = _array(documents, "documents", (B, N), torch.int32, on.device)
-        pre = _array(prefix, "prefix", (B,), torch.int32, on.device)
-        need = 0
-        if workspace is None:
-            need = _prompt_bytes(B, Hq, Hkv, T, N, d, q.dtype, window, documents is not None, on.device)
-        ws, ws_bytes, keep = _scratch(workspace, need, on.device)
-        check(_lib.load().santapp_prompt_attention(
-            ctypes.byref(sc), ctypes.byref(qr), ctypes.byref(kr), ctypes.byref(vr), code, B, Hq, Hkv, T, N, d,
-            int(bool(causal)), int(offset), docs, pre, ctypes.byref(orr), ws, ws_bytes, on.stream))
-        _hold(keep, workspace, stream)
+    device, current, s = _on(q, "q", stream)
+    if q.dim() != 4 or K.dim() != 4:
+        _fail("q and K must be [B, H, tokens, d]")
+    shape = q.shape
+    B, Hq, T, d = shape
+    Hkv, N = K.shape[1], K.shape[2]
+    dtype = q.dtype
+    if K.dtype != dtype or V.dtype != dtype:
+        _fail(f"q, K and V must have one type, got {dtype}, {K.dtype}, {V.dtype}")
+    code = _code(q, "q")
+    if offset is None:
+        offset = N - T if N >= T or causal else 0
+    if out is None:
+        out = torch.empty_like(q)  # q's order of dimensions where q is dense
+        if stream is not None:
+            out.record_stream(stream)
+    elif out.dtype != dtype:
+        _fail(f"out has dtype {out.dtype}, expected {dtype}")
+    keys = (B, Hkv, N, d)
+    qr, kr, vr = _rows(q, "q", shape, device), _rows(K, "K", keys, device), _rows(V, "V", keys, device)
+    orr = _rows(out, "out", shape, device)
+    docs = _array(documents, "documents", (B, N), torch.int32, device)
+    pre = _array(prefix, "prefix", (B,), torch.int32, device)
+    lib = _lib.load()
+
+    def size():
+        n = ctypes.c_size_t()
+        _call(device, current, lib.santapp_prompt_workspace_bytes, B, Hq, Hkv, T, N, d, code, window, docs is not None, n)
+        return n.value
+    ws, ws_bytes, hold = _scratch(workspace, size, device, stream)
+    _call(device, current, lib.santapp_prompt_attention, _score(scale, softcap, slopes, window, Hq, device), qr, kr, vr, code,
+          B, Hq, Hkv, T, N, d, bool(causal), offset, docs, pre, orr, ws, ws_bytes, s)
     return out
-
-
-def _dense(t: torch.Tensor) -> bool:
-    """Whether the view covers its memory without gaps or repeats, rows whole."""
-    n = 1
-    for size, stride in sorted(zip(t.shape, t.stride()), key=lambda x: (x[1], x[0])):
-        if size != 1 and stride != n:
-            return False
-        n *= size
-    return t.stride(3) == 1
-
-
-def _hold(keep, given, stream):
-    """A workspace made for a call on a stream that is not the current one must
-    not be given out again before that stream has passed it."""
-    if keep is not None and given is None and stream is not None:
-        keep.record_stream(stream)
 
 
 def prefix_workspace(P: int, S: int, Hq: int, Hkv: int, N: int, T: int, d: int, dtype: torch.dtype = torch.bfloat16,
                      device="cuda") -> torch.Tensor:
     """Workspace of :func:`prefix_decode` at these sizes (uninitialised)."""
-    return torch.empty(max(_prefix_bytes(P, S, Hq, Hkv, N, T, d, dtype, torch.device(device)), 1), dtype=torch.uint8,
-                       device=device)
-
-
-def _prefix_bytes(P, S, Hq, Hkv, N, T, d, dtype, device) -> int:
     n = ctypes.c_size_t()
     with torch.cuda.device(device):
-        check(_lib.load().santapp_prefix_workspace_bytes(P, S, Hq, Hkv, N, T, d,
-                                                         _lib.BF16 if dtype == torch.bfloat16 else _lib.FP32,
-                                                         ctypes.byref(n)))
-    return n.value
+        check(_lib.load().santapp_prefix_workspace_bytes(P, S, Hq, Hkv, N, T, d, _dtype(dtype), ctypes.byref(n)))
+    return torch.empty(max(n.value, 1), dtype=torch.uint8, device=device)
 
 
 def prefix_decode(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, suffix_K: Optional[torch.Tensor] = None,
@@ -370,49 +330,51 @@ def prefix_decode(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, suffix_K: O
     ``lengths[b]`` rows of its own suffix ``[B, Hkv, capacity, d]``.  Scores as in
     :func:`prompt_attention`; for ``window`` and ``slopes`` the query stands at
     ``positions[b]`` (int32; default: its last row)."""
-    with _On(q, "q", stream) as on:
-        if q.dim() != 3 or K.dim() != 4:
-            _fail("q must be [B, Hq, d], K [P, Hkv, N, d]")
-        B, Hq, d = q.shape
-        P, Hkv, N = K.shape[:3]
-        if P < 1 or B % P:
-            _fail(f"{B} sequences over {P} prompts")
-        if V.dtype != K.dtype:
-            _fail("K and V must have one type")
-        qp = _array(q, "q", (B, Hq, d), torch.float32, on.device)
-        code = _code(K, "K")
-        kr, vr = _rows(K, "K", (P, Hkv, N, d), on.device), _rows(V, "V", (P, Hkv, N, d), on.device)
-        sk = sv = None
-        if suffix_K is None:
-            if T or lengths is not None:
-                _fail("suffix rows requested without a suffix buffer")
-            T = 0
-        else:
-            if suffix_V is None or suffix_K.dtype != K.dtype or suffix_V.dtype != K.dtype:
-                _fail("suffix_K and suffix_V must have the type of K")
-            if suffix_K.dim() != 4:
-                _fail("suffix_K must be [B, Hkv, capacity, d]")
-            cap = suffix_K.shape[2]
-            sk = ctypes.byref(_rows(suffix_K, "suffix_K", (B, Hkv, cap, d), on.device))
-            sv = ctypes.byref(_rows(suffix_V, "suffix_V", (B, Hkv, cap, d), on.device))
-            T = cap if T is None else int(T)
-            if T < 0 or T > cap:
-                _fail(f"T={T} outside the suffix buffer's {cap} rows")
-        if out is None:
-            out = torch.empty((B, Hq, d), dtype=torch.float32, device=on.device)
-        op = _array(out, "out", (B, Hq, d), torch.float32, on.device)
-        if any(_same_memory(out, x) for x in (q, K, V, suffix_K, suffix_V) if x is not None):
-            _fail("out must not overlap q or the caches")
-        sc = _score(scale, softcap, slopes, window, Hq, on.device)
-        lens = _array(lengths, "lengths", (B,), torch.int32, on.device)
-        plens = _array(prefix_lengths, "prefix_lengths", (P,), torch.int32, on.device)
-        pos = _array(positions, "positions", (B,), torch.int32, on.device)
-        need = 0
-        if workspace is None:
-            need = _prefix_bytes(P, B // P, Hq, Hkv, N, T, d, K.dtype, on.device)
-        ws, ws_bytes, keep = _scratch(workspace, need, on.device)
-        check(_lib.load().santapp_prefix_decode(
-            ctypes.byref(sc), qp, ctypes.byref(kr), ctypes.byref(vr), code, P, B // P, Hq, Hkv, N, d, plens, sk, sv, T,
-            lens, pos, op, ws, ws_bytes, on.stream))
-        _hold(keep, workspace, stream)
+    device, current, s = _on(q, "q", stream)
+    if q.dim() != 3 or K.dim() != 4:
+        _fail("q must be [B, Hq, d], K [P, Hkv, N, d]")
+    shape = q.shape
+    B, Hq, d = shape
+    P, Hkv, N, _ = K.shape
+    if P < 1 or B % P:
+        _fail(f"{B} sequences over {P} prompts")
+    S = B // P
+    dtype = K.dtype
+    if V.dtype != dtype:
+        _fail("K and V must have one type")
+    code = _code(K, "K")
+    sk = sv = None
+    if suffix_K is None:
+        if T or lengths is not None:
+            _fail("suffix rows requested without a suffix buffer")
+        T = 0
+    else:
+        if suffix_V is None or suffix_K.dtype != dtype or suffix_V.dtype != dtype:
+            _fail("suffix_K and suffix_V must have the type of K")
+        if suffix_K.dim() != 4:
+            _fail("suffix_K must be [B, Hkv, capacity, d]")
+        cap = suffix_K.shape[2]
+        held = (B, Hkv, cap, d)
+        sk, sv = _rows(suffix_K, "suffix_K", held, device), _rows(suffix_V, "suffix_V", held, device)
+        if T is None:
+            T = cap
+        elif T < 0 or T > cap:
+            _fail(f"T={T} outside the suffix buffer's {cap} rows")
+    if out is None:
+        out = torch.empty(shape, dtype=torch.float32, device=device)
+        if stream is not None:
+            out.record_stream(stream)
+    keys = (P, Hkv, N, d)
+    kr, vr = _rows(K, "K", keys, device), _rows(V, "V", keys, device)
+    lib = _lib.load()
+
+    def size():
+        n = ctypes.c_size_t()
+        _call(device, current, lib.santapp_prefix_workspace_bytes, P, S, Hq, Hkv, N, T, d, code, n)
+        return n.value
+    ws, ws_bytes, hold = _scratch(workspace, size, device, stream)
+    _call(device, current, lib.santapp_prefix_decode, _score(scale, softcap, slopes, window, Hq, device),
+          _array(q, "q", shape, torch.float32, device), kr, vr, code, P, S, Hq, Hkv, N, d, _array(prefix_lengths, "prefix_lengths", (P,), torch.int32, device), sk, sv, T,
+          _array(lengths, "lengths", (B,), torch.int32, device), _array(positions, "positions", (B,), torch.int32, device),
+          _array(out, "out", shape, torch.float32, device), ws, ws_bytes, s)
     return out

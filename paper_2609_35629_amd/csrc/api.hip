@@ -489,11 +489,30 @@ using namespace santapp;
 
 namespace {
 
+// The bytes between a view's first and last element.
+struct Span {
+    const char *name, *lo, *hi;
+    Rows rows;
+};
+
+// `out` must meet none of the inputs; with `self`, it may be that input itself
+// (the same rows).
+santapp_status check_apart(const Span& out, const Span* in, int n, const Span* self = nullptr) {
+    for (int i = 0; i < n; ++i) {
+        if (out.lo >= in[i].hi || in[i].lo >= out.hi) continue;
+        if (&in[i] == self && out.lo == in[i].lo && out.hi == in[i].hi && out.rows.b == in[i].rows.b &&
+            out.rows.h == in[i].rows.h && out.rows.t == in[i].rows.t)
+            continue;
+        return fail(SANTAPP_EINVAL, "%s overlaps %s", out.name, in[i].name);
+    }
+    return SANTAPP_OK;
+}
+
 // A view of B x heads x tokens rows of d elements as the kernels take it
 // (distances in bytes, 0 along dimensions of one entry).  `out`: no two rows
 // may share bytes.
 santapp_status check_rows(const santapp_rows* v, const char* name, santapp_dtype dt, long long B, long long H,
-                          long long T, int d, bool out, Rows* r) {
+                          long long T, int d, bool out, Rows* r, Span* span = nullptr) {
     if (!v || !v->data) return fail(SANTAPP_EINVAL, "%s is NULL", name);
     if (!aligned16(v->data)) return fail(SANTAPP_EINVAL, "%s must be 16-byte aligned", name);
     const long long es = static_cast<long long>(elem_size(dt));
@@ -509,6 +528,12 @@ santapp_status check_rows(const santapp_rows* v, const char* name, santapp_dtype
     r->b = dim[0].stride * es;
     r->h = dim[1].stride * es;
     r->t = dim[2].stride * es;
+    if (span) {
+        span->name = name;
+        span->lo = r->p;
+        span->hi = r->p + (B - 1) * r->b + (H - 1) * r->h + (T - 1) * r->t + d * es;
+        span->rows = *r;
+    }
     if (out) {
         std::sort(dim, dim + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
         long long extent = d;  // elements from the first to the end of the last row so far
@@ -523,8 +548,8 @@ santapp_status check_rows(const santapp_rows* v, const char* name, santapp_dtype
 
 // Keys or values: rows within the reach of the kernels' offsets.
 santapp_status check_keys(const santapp_rows* v, const char* name, santapp_dtype dt, long long B, long long H, long long T,
-                          int d, Rows* r) {
-    if (santapp_status st = check_rows(v, name, dt, B, H, T, d, false, r)) return st;
+                          int d, Rows* r, Span* span) {
+    if (santapp_status st = check_rows(v, name, dt, B, H, T, d, false, r, span)) return st;
     if (r->t > kMaxRowStep) return fail(SANTAPP_ELIMIT, "%s: rows more than %lld bytes apart", name, kMaxRowStep);
     return SANTAPP_OK;
 }
@@ -1266,8 +1291,10 @@ santapp_status santapp_rope(const santapp_rotation* rotation, const santapp_rows
     if (static_cast<long long>(B) * T > kMaxRows || static_cast<long long>(B) * T * H > 8 * kMaxRows)
         return fail(SANTAPP_ELIMIT, "too many rows");
     Rows xr, yr;
-    if (santapp_status st = check_rows(x, "x", x_dtype, B, H, T, d, false, &xr)) return st;
-    if (santapp_status st = check_rows(out, "out", out_dtype, B, H, T, d, true, &yr)) return st;
+    Span in, to;
+    if (santapp_status st = check_rows(x, "x", x_dtype, B, H, T, d, false, &xr, &in)) return st;
+    if (santapp_status st = check_rows(out, "out", out_dtype, B, H, T, d, true, &yr, &to)) return st;
+    if (santapp_status st = check_apart(to, &in, 1, x_dtype == out_dtype ? &in : nullptr)) return st;
     RopeArgs a{};
     a.s[0] = rope_stream(xr, x_dtype, yr, out_dtype, H, true, false);
     a.freqs = rotation->freqs;
@@ -1304,15 +1331,25 @@ santapp_status santapp_rope_append(const santapp_rotation* rotation, const santa
         return fail(SANTAPP_ELIMIT, "too many rows");
     Rows qr, qo, kr, vr, ck, cv;
     RopeArgs a{};
+    Span in[5], to[3];  // inputs k, v, q and the outputs that are checked; outputs
+    int n = 2;
     if (q) {
-        if (santapp_status st = check_rows(q, "q", q_dtype, B, Hq, T, d, false, &qr)) return st;
-        if (santapp_status st = check_rows(q_out, "q_out", q_out_dtype, B, Hq, T, d, true, &qo)) return st;
+        if (santapp_status st = check_rows(q, "q", q_dtype, B, Hq, T, d, false, &qr, &in[n])) return st;
+        if (santapp_status st = check_rows(q_out, "q_out", q_out_dtype, B, Hq, T, d, true, &qo, &to[0])) return st;
+        ++n;
         a.s[0] = rope_stream(qr, q_dtype, qo, q_out_dtype, Hq, true, false);
     }
-    if (santapp_status st = check_rows(k, "k", kv_dtype, B, Hkv, T, d, false, &kr)) return st;
-    if (santapp_status st = check_rows(v, "v", kv_dtype, B, Hkv, T, d, false, &vr)) return st;
-    if (santapp_status st = check_rows(cache_K, "cache_K", cache_dtype, B, Hkv, capacity, d, true, &ck)) return st;
-    if (santapp_status st = check_rows(cache_V, "cache_V", cache_dtype, B, Hkv, capacity, d, true, &cv)) return st;
+    if (santapp_status st = check_rows(k, "k", kv_dtype, B, Hkv, T, d, false, &kr, &in[0])) return st;
+    if (santapp_status st = check_rows(v, "v", kv_dtype, B, Hkv, T, d, false, &vr, &in[1])) return st;
+    if (santapp_status st = check_rows(cache_K, "cache_K", cache_dtype, B, Hkv, capacity, d, true, &ck, &to[1])) return st;
+    if (santapp_status st = check_rows(cache_V, "cache_V", cache_dtype, B, Hkv, capacity, d, true, &cv, &to[2])) return st;
+    if (q) {
+        if (santapp_status st = check_apart(to[0], in, n, q_dtype == q_out_dtype ? &in[2] : nullptr)) return st;
+        in[n++] = to[0];
+    }
+    if (santapp_status st = check_apart(to[1], in, n)) return st;
+    in[n++] = to[1];
+    if (santapp_status st = check_apart(to[2], in, n)) return st;
     a.s[1] = rope_stream(kr, kv_dtype, ck, cache_dtype, Hkv, true, true);
     a.s[2] = rope_stream(vr, kv_dtype, cv, cache_dtype, Hkv, false, true);
     a.freqs = rotation->freqs;
@@ -1379,12 +1416,15 @@ santapp_status santapp_prompt_attention(const santapp_score* score, const santap
         return fail(SANTAPP_EINVAL, "queries %d .. %lld are not tokens of the sequence's %d", offset,
                     static_cast<long long>(offset) + T, N);
     if (T == 0) return ok();
-    if (santapp_status st = check_rows(q, "q", dtype, B, Hq, T, d, false, &a.q)) return st;
-    if (santapp_status st = check_rows(out, "out", dtype, B, Hq, T, d, true, &a.out)) return st;
+    Span in[3], to;
+    int n = 1;
+    if (santapp_status st = check_rows(q, "q", dtype, B, Hq, T, d, false, &a.q, &in[0])) return st;
+    if (santapp_status st = check_rows(out, "out", dtype, B, Hq, T, d, true, &a.out, &to)) return st;
     if (N > 0) {
-        if (santapp_status st = check_keys(K, "K", dtype, B, Hkv, N, d, &a.K)) return st;
-        if (santapp_status st = check_keys(V, "V", dtype, B, Hkv, N, d, &a.V)) return st;
+        if (santapp_status st = check_keys(K, "K", dtype, B, Hkv, N, d, &a.K, &in[n++])) return st;
+        if (santapp_status st = check_keys(V, "V", dtype, B, Hkv, N, d, &a.V, &in[n++])) return st;
     }
+    if (santapp_status st = check_apart(to, in, n)) return st;
     a.causal = causal != 0;
     a.offset = offset;
     a.documents = documents;
@@ -1440,14 +1480,19 @@ santapp_status santapp_prefix_decode(const santapp_score* score, const float* q,
     if (!aligned4(prefix_lengths) || !aligned4(lengths) || !aligned4(positions) || !aligned4(score->slopes))
         return fail(SANTAPP_EINVAL, "lengths, positions and slopes must be 4-byte aligned");
     const long long B = static_cast<long long>(P) * S;
+    const size_t qbytes = static_cast<size_t>(B) * Hq * d * sizeof(float);
+    const Span to = {"out", reinterpret_cast<const char*>(out), reinterpret_cast<const char*>(out) + qbytes, {}};
+    Span in[5] = {{"q", reinterpret_cast<const char*>(q), reinterpret_cast<const char*>(q) + qbytes, {}}};
+    int n = 1;
     if (N > 0) {
-        if (santapp_status st = check_keys(K, "K", dtype, P, Hkv, N, d, &a.K)) return st;
-        if (santapp_status st = check_keys(V, "V", dtype, P, Hkv, N, d, &a.V)) return st;
+        if (santapp_status st = check_keys(K, "K", dtype, P, Hkv, N, d, &a.K, &in[n++])) return st;
+        if (santapp_status st = check_keys(V, "V", dtype, P, Hkv, N, d, &a.V, &in[n++])) return st;
     }
     if (T > 0) {
-        if (santapp_status st = check_keys(suffix_K, "suffix_K", dtype, B, Hkv, T, d, &a.sK)) return st;
-        if (santapp_status st = check_keys(suffix_V, "suffix_V", dtype, B, Hkv, T, d, &a.sV)) return st;
+        if (santapp_status st = check_keys(suffix_K, "suffix_K", dtype, B, Hkv, T, d, &a.sK, &in[n++])) return st;
+        if (santapp_status st = check_keys(suffix_V, "suffix_V", dtype, B, Hkv, T, d, &a.sV, &in[n++])) return st;
     }
+    if (santapp_status st = check_apart(to, in, n)) return st;
     a.q = q;
     a.out = out;
     a.prefix_lengths = prefix_lengths;

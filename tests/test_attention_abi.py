@@ -2,6 +2,7 @@
 host-side checks that answer before anything is launched (no GPU needed; the
 addresses are never dereferenced)."""
 import ctypes
+import functools
 import os
 import subprocess
 import sys
@@ -59,6 +60,9 @@ def test_rope_refusals():
     refused(call(out=rows(t=56)), "rows overlap")       # closer than a row
     refused(call(out=rows(h=128, t=128)), "rows overlap")
     refused(call(out=rows(t=0)), "rows overlap")
+    refused(call(out=rows(FAKE + 128)), "out overlaps x")
+    refused(call(out=rows(t=256)), "out overlaps x")
+    refused(call(od=FP32), "out overlaps x")            # in place, but of another type
     refused(call(B=1 << 16, T=1 << 16), "too many rows", _lib.ELIMIT)
     assert call(T=0, x=rows(None)) == _lib.OK           # nothing to do
     assert L.santapp_rope(None, rows(), BF16, 1, 1, 1, 64, None, 0, rows(), BF16, None) == _lib.EINVAL
@@ -66,6 +70,7 @@ def test_rope_refusals():
 
 def test_rope_append_refusals():
     L = _lib.load()
+    far = [FAKE + (i << 24) for i in range(8)]
 
     def call(q=None, Hq=0, k=None, v=None, kd=BF16, ck=None, cv=None, cd=BF16, cap=16, B=1, Hkv=2, T=4, d=64, at=None,
              at0=0, qo=None, qd=BF16, od=FP32):
@@ -89,6 +94,12 @@ def test_rope_append_refusals():
     refused(call(ck=rows(t=32)), "cache_K: rows overlap")
     refused(call(cv=rows(h=32)), "cache_V: rows overlap")  # (64: two heads side by side in a token of 128)
     refused(call(d=32), "head dim", _lib.ELIMIT)
+    apart = dict(k=rows(far[0]), v=rows(far[1]), ck=rows(far[2]), cv=rows(far[3]))
+    refused(call(**dict(apart, ck=rows(far[0] + 16))), "cache_K overlaps k")
+    refused(call(**dict(apart, cv=rows(far[1]))), "cache_V overlaps v")
+    refused(call(**dict(apart, cv=rows(far[2]))), "cache_V overlaps cache_K")
+    refused(call(**apart, q=rows(far[4]), Hq=2, qo=rows(far[4])), "q_out overlaps q")  # of another type
+    refused(call(**apart, q=rows(far[4]), Hq=2, qo=rows(far[2])), "cache_K overlaps q_out")
     assert call(T=0) == _lib.OK
 
 
@@ -127,6 +138,9 @@ def test_prompt_refusals():
     refused(call(V=rows(t=4)), "V: distances")
     refused(call(V=rows(t=1 << 30)), "bytes apart", _lib.ELIMIT)
     refused(call(out=rows(t=0)), "out: rows overlap")
+    refused(call(), "out overlaps q")
+    call = functools.partial(call, out=rows(FAKE + (1 << 28)))
+    refused(call(K=rows(FAKE + (1 << 28))), "out overlaps K")
     refused(call(ws=ODD), "workspace must be 16-byte aligned")
     n = ctypes.c_size_t()
     args = (1, 28, 4, 1, 32768, 128, BF16, 0, 1)
@@ -167,6 +181,9 @@ def test_prefix_refusals():
     refused(call(K=rows(None)), "K is NULL")
     refused(call(sK=rows(None)), "suffix_K is NULL")
     refused(call(sV=rows(ODD)), "suffix_V must be 16-byte aligned")
+    refused(call(), "out overlaps q")
+    call = functools.partial(call, out=FAKE + (1 << 28))
+    refused(call(sV=rows(FAKE + (1 << 28))), "out overlaps suffix_V")
     n = ctypes.c_size_t()
     assert L.santapp_prefix_workspace_bytes(1, 2, 4, 2, 16, 8, 64, BF16, ctypes.byref(n)) == _lib.OK and n.value > 0
     refused(call(wb=n.value - 1), "workspace of", _lib.EWORKSPACE)
