@@ -138,6 +138,32 @@ constexpr int variant_of(long long rows) { return rows <= 32 ? 0 : rows <= 64 ? 
 constexpr int row_waves(int v) { return v == 0 ? 1 : v == 1 ? 2 : 4; }
 // fp32 tiles are twice as large: two waves over keys fill the LDS
 constexpr int key_waves(int v, bool f32) { return v == 0 ? (f32 ? 2 : 4) : v == 1 ? 2 : 1; }
-inline int tile_keys(int v, bool f32) { return f32 ? 32 * key_waves(v, true) : 32 * (key_waves(v, false) == 1 ? 2 : key_waves(v, false)); }
+
+template <typename F>
+auto with_shape(int v, int d, bool f32, int terms, F&& f) {
+    auto shape = [&](auto wr, auto wk32, auto wk16) {
+        constexpr int WR = decltype(wr)::value, W32 = decltype(wk32)::value, W16 = decltype(wk16)::value;
+        if (f32) return d == 64 ? f(Shape<float, 64, 1, WR, W32>{}) : f(Shape<float, 128, 1, WR, W32>{});
+        if (terms == 1) return d == 64 ? f(Shape<bf16_t, 64, 1, WR, W16>{}) : f(Shape<bf16_t, 128, 1, WR, W16>{});
+        return d == 64 ? f(Shape<bf16_t, 64, 3, WR, W16>{}) : f(Shape<bf16_t, 128, 3, WR, W16>{});
+    };
+    using std::integral_constant;
+    if (v == 0)
+        return shape(integral_constant<int, row_waves(0)>{}, integral_constant<int, key_waves(0, true)>{},
+                     integral_constant<int, key_waves(0, false)>{});
+    if (v == 1)
+        return shape(integral_constant<int, row_waves(1)>{}, integral_constant<int, key_waves(1, true)>{},
+                     integral_constant<int, key_waves(1, false)>{});
+    return shape(integral_constant<int, row_waves(2)>{}, integral_constant<int, key_waves(2, true)>{},
+                 integral_constant<int, key_waves(2, false)>{});
+}
+
+// Keys of a tile, and workgroups a compute unit holds, of a variant's kernel.
+inline int tile_keys(int v, bool f32) {
+    return with_shape(v, 128, f32, 1, [](auto s) { return decltype(s)::BK; });
+}
+inline int per_cu(int v, int d, bool f32, int terms) {
+    return with_shape(v, d, f32, terms, [](auto s) { return decltype(s)::kPerCu; });
+}
 
 }  // namespace santapp

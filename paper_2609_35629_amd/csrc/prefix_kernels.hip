@@ -25,7 +25,7 @@ struct PrefixShape {
     static constexpr int kPerCu = Prompt::kPerCu < Suffix::kPerCu ? Prompt::kPerCu : Suffix::kPerCu;
 };
 
-template <typename T, int D, int WR, int WK, bool EXTRA>
+template <typename T, int D, int WR, int WK, int MODE>
 __global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) void k_prefix(PrefixArgs a) {
     using PS = PrefixShape<T, D, WR, WK>;
     using SH = typename PS::Prompt;
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) 
                 x.hi = static_cast<int>(min(max(pos + a.score.window, 0ll), static_cast<long long>(seg.n)));
             }
             x.doc = 0;
-            x.slope = EXTRA && a.score.slopes ? a.score.slopes[h] * 1.44269504088896341f : 0.f;
+            x.slope = (MODE & kExtra) != 0 && a.score.slopes ? a.score.slopes[h] * 1.44269504088896341f : 0.f;
             return x;
         };
         auto head = [&](int r) {
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) 
             else
                 store4(a.out + head(r) * D + dim, v, inverse_sum(l));
         };
-        attend<T, D, NT, WR, WK, EXTRA, true>(seg, a.score, nullptr, nullptr, split, a.part.splits, buf0, buf1, rowinfo, qrow,
+        attend<T, D, NT, WR, WK, MODE, true>(seg, a.score, nullptr, nullptr, split, a.part.splits, buf0, buf1, rowinfo, qrow,
                                             emit);
         return;
     }
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) 
             x.hi = static_cast<int>(min(max(pos + a.score.window, 0ll), static_cast<long long>(seg.n)));
         }
         x.doc = 0;
-        x.slope = EXTRA && a.score.slopes ? a.score.slopes[kv * a.G + min(r0 + r, a.G - 1)] * 1.44269504088896341f : 0.f;
+        x.slope = (MODE & kExtra) != 0 && a.score.slopes ? a.score.slopes[kv * a.G + min(r0 + r, a.G - 1)] * 1.44269504088896341f : 0.f;
         return x;
     };
     auto head = [&](int r) { return static_cast<long long>(b) * Hq + kv * a.G + r0 + r; };
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) 
         else
             store4(a.out + head(r) * D + dim, v, inverse_sum(l));
     };
-    attend<T, D, NT, WR * WK / SK, SK, EXTRA, true>(seg, a.score, nullptr, nullptr, split, a.spart.splits, buf0, buf1,
+    attend<T, D, NT, WR * WK / SK, SK, MODE, true>(seg, a.score, nullptr, nullptr, split, a.spart.splits, buf0, buf1,
                                                        rowinfo, qrow, emit);
 }
 
@@ -137,22 +137,19 @@ hipError_t launch(const PrefixArgs& a, hipStream_t s) {
     const long long n = static_cast<long long>(a.P) * a.Hkv * a.row_blocks * a.part.splits +
                         static_cast<long long>(a.P) * a.S * a.Hkv * a.srow_blocks * a.spart.splits;
     const dim3 grid(static_cast<unsigned>(n));
-    const bool extra = a.score.capped || a.score.slopes;
-#define SANTAPP_PREFIX(V)                                                                                      \
-    case V:                                                                                                    \
-        if (extra)                                                                                             \
-            k_prefix<T, D, row_waves(V), key_waves(V, f32), true>                                              \
-                <<<grid, 64 * row_waves(V) * key_waves(V, f32), 0, s>>>(a);                                    \
-        else                                                                                                   \
-            k_prefix<T, D, row_waves(V), key_waves(V, f32), false>                                             \
-                <<<grid, 64 * row_waves(V) * key_waves(V, f32), 0, s>>>(a);                                    \
-        break;
-    switch (a.variant) {
-        SANTAPP_PREFIX(0)
-        SANTAPP_PREFIX(1)
-        SANTAPP_PREFIX(2)
-    }
-#undef SANTAPP_PREFIX
+    auto run = [&](auto variant) {
+        constexpr int V = decltype(variant)::value, WK = key_waves(V, f32);
+        if (a.score.capped || a.score.slopes)
+            k_prefix<T, D, row_waves(V), WK, kExtra><<<grid, 64 * row_waves(V) * WK, 0, s>>>(a);
+        else
+            k_prefix<T, D, row_waves(V), WK, 0><<<grid, 64 * row_waves(V) * WK, 0, s>>>(a);
+    };
+    if (a.variant == 0)
+        run(std::integral_constant<int, 0>{});
+    else if (a.variant == 1)
+        run(std::integral_constant<int, 1>{});
+    else
+        run(std::integral_constant<int, 2>{});
     if (hipError_t e = hipGetLastError()) return e;
     if (a.part.splits + a.spart.splits > 1) {
         k_prefix_join<D><<<dim3(static_cast<unsigned>(a.P * a.S * a.Hkv * a.G)), kJoinThreads, 0, s>>>(a);
@@ -168,26 +165,31 @@ size_t plan_prefix(PrefixArgs& a, int cus, char* ws) {
     const long long R = static_cast<long long>(a.S) * a.G, pairs = static_cast<long long>(a.P) * a.Hkv;
     a.variant = variant_of(R);
     const int bm = 32 * row_waves(a.variant), bk = tile_keys(a.variant, f32);
-    a.row_blocks = a.N > 0 ? static_cast<int>((R + bm - 1) / bm) : 0;
-    const long long blocks = pairs * a.row_blocks;
-    long long splits = 0;
-    if (blocks > 0) {
-        const long long tiles = (a.N + bk - 1) / bk;
-        splits = (2 * cus + blocks - 1) / blocks;
-        if (splits > tiles / 2) splits = tiles / 2;
-        splits = splits < 1 ? 1 : splits > 256 ? 256 : splits;
-    }
-    a.part.splits = static_cast<int>(splits);
+    const long long slots = static_cast<long long>(per_cu(a.variant, a.d, f32, f32 ? 1 : 3)) * cus;
+    // the suffixes: a block per 32 heads (times the waves over rows) each, split
+    // while they are few
     const int kw = suffix_key_waves(a.variant, f32);
     const int sbm = 32 * (row_waves(a.variant) * key_waves(a.variant, f32) / kw);
     a.srow_blocks = a.T > 0 ? (a.G + sbm - 1) / sbm : 0;
+    const long long sblocks = pairs * a.S * a.srow_blocks;
     a.spart.splits = 0;
     if (a.T > 0) {
-        const long long sblocks = pairs * a.S * a.srow_blocks;
         const long long tiles = (a.T + 32 * kw - 1) / (32 * kw);
-        long long k = cus / sblocks;
-        k = k > tiles / 2 ? tiles / 2 : k;
+        long long k = slots / 8 / sblocks;
+        k = k > tiles ? tiles : k;
         a.spart.splits = static_cast<int>(k < 1 ? 1 : k > 64 ? 64 : k);
+    }
+    // the prompts: as many splits as leave every workgroup slot one block, the
+    // suffixes' included
+    a.row_blocks = a.N > 0 ? static_cast<int>((R + bm - 1) / bm) : 0;
+    const long long blocks = pairs * a.row_blocks;
+    a.part.splits = 0;
+    if (blocks > 0) {
+        const long long tiles = (a.N + bk - 1) / bk;
+        const long long left = slots - sblocks * a.spart.splits;
+        long long k = (left > slots / 2 ? left : slots) / blocks;
+        if (k > tiles) k = tiles;
+        a.part.splits = static_cast<int>(k < 1 ? 1 : k > 256 ? 256 : k);
     }
     if (a.part.splits + a.spart.splits <= 1) return 0;
     size_t at = 0;

@@ -23,7 +23,7 @@ __global__ __launch_bounds__(256) void k_doc_ranges(const int* docs, int B, int 
     if (i % kDocTile == 0) ranges[row * nr + r] = make_int2(lo, hi);
 }
 
-template <typename T, int D, int WR, int WK, bool EXTRA>
+template <typename T, int D, int WR, int WK, int MODE>
 __global__ __launch_bounds__(64 * WR * WK, (Shape<T, D, 1, WR, WK>::kPerCu)) void k_prompt(PromptArgs a) {
     using SH = Shape<T, D, 1, WR, WK>;
     __shared__ __align__(16) char buf0[SH::kBuf];
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Shape<T, D, 1, WR, WK>::kPerCu)) voi
     seg.kt = a.K.t;
     seg.vt = a.V.t;
     seg.n = a.N;
-    const int* docs = EXTRA && a.documents ? a.documents + static_cast<long long>(b) * a.N : nullptr;
+    const int* docs = (MODE & kDocs) != 0 ? a.documents + static_cast<long long>(b) * a.N : nullptr;
     const int prefix = a.prefix ? a.prefix[b] : 0;
     auto rowinfo = [&](int r) {
         RowInfo x;
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Shape<T, D, 1, WR, WK>::kPerCu)) voi
         x.lo = lo;
         x.hi = hi;
         x.doc = docs ? docs[x.pos] : 0;
-        x.slope = EXTRA && a.score.slopes ? a.score.slopes[h] * 1.44269504088896341f : 0.f;
+        x.slope = (MODE & kExtra) != 0 && a.score.slopes ? a.score.slopes[h] * 1.44269504088896341f : 0.f;
         return x;
     };
     auto qrow = [&](int r) {
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Shape<T, D, 1, WR, WK>::kPerCu)) voi
         store4(reinterpret_cast<T*>(p) + dim, v, inverse_sum(l));
     };
     const int2* ranges = docs ? a.doc_range + static_cast<long long>(b) * ((a.N + kDocTile - 1) / kDocTile) : nullptr;
-    attend<T, D, 1, WR, WK, EXTRA, sizeof(T) == 4>(seg, a.score, docs, ranges, split, a.part.splits, buf0, buf1, rowinfo,
+    attend<T, D, 1, WR, WK, MODE, sizeof(T) == 4>(seg, a.score, docs, ranges, split, a.part.splits, buf0, buf1, rowinfo,
                                                  qrow, emit);
 }
 
@@ -100,22 +100,25 @@ hipError_t launch(const PromptArgs& a, hipStream_t s) {
         if (hipError_t e = hipGetLastError()) return e;
     }
     const dim3 grid(static_cast<unsigned>(BH * a.part.splits * a.row_blocks));
-    const bool extra = a.score.capped || a.score.slopes || a.documents;
-#define SANTAPP_PROMPT(V)                                                                                      \
-    case V:                                                                                                    \
-        if (extra)                                                                                             \
-            k_prompt<T, D, row_waves(V), key_waves(V, f32), true>                                              \
-                <<<grid, 64 * row_waves(V) * key_waves(V, f32), 0, s>>>(a);                                    \
-        else                                                                                                   \
-            k_prompt<T, D, row_waves(V), key_waves(V, f32), false>                                             \
-                <<<grid, 64 * row_waves(V) * key_waves(V, f32), 0, s>>>(a);                                    \
-        break;
-    switch (a.variant) {
-        SANTAPP_PROMPT(0)
-        SANTAPP_PROMPT(1)
-        SANTAPP_PROMPT(2)
-    }
-#undef SANTAPP_PROMPT
+    auto run = [&](auto variant, auto mode) {
+        constexpr int V = decltype(variant)::value, WK = key_waves(V, f32);
+        k_prompt<T, D, row_waves(V), WK, decltype(mode)::value><<<grid, 64 * row_waves(V) * WK, 0, s>>>(a);
+    };
+    auto modes = [&](auto variant) {
+        using std::integral_constant;
+        if (a.documents)
+            a.score.capped || a.score.slopes ? run(variant, integral_constant<int, kExtra | kDocs>{})
+                                             : run(variant, integral_constant<int, kDocs>{});
+        else
+            a.score.capped || a.score.slopes ? run(variant, integral_constant<int, kExtra>{})
+                                             : run(variant, integral_constant<int, 0>{});
+    };
+    if (a.variant == 0)
+        modes(std::integral_constant<int, 0>{});
+    else if (a.variant == 1)
+        modes(std::integral_constant<int, 1>{});
+    else
+        modes(std::integral_constant<int, 2>{});
     if (hipError_t e = hipGetLastError()) return e;
     if (a.part.splits > 1) {
         k_prompt_join<T, D><<<dim3(static_cast<unsigned>(BH * R)), kJoinThreads, 0, s>>>(a);
@@ -130,16 +133,19 @@ size_t plan_prompt(PromptArgs& a, int cus, char* ws) {
     const bool f32 = a.dtype == SANTAPP_FP32;
     const long long R = static_cast<long long>(a.T) * a.G, BH = static_cast<long long>(a.B) * a.Hkv;
     a.variant = variant_of(R);
-    const int bm = 32 * row_waves(a.variant), bk = tile_keys(a.variant, f32);
-    a.row_blocks = static_cast<int>((R + bm - 1) / bm);
-    // few blocks of rows: their keys are split until two workgroups per compute
-    // unit have work, two tiles each at least
-    const long long blocks = BH * a.row_blocks;
+    // blocks differ in length under a mask: of fewer than four per compute unit
+    // the longest set the time, so smaller ones are taken
+    auto blocks_of = [&](int v) { return BH * ((R + 32 * row_waves(v) - 1) / (32 * row_waves(v))); };
+    while (a.variant > 0 && blocks_of(a.variant) < 4ll * cus && blocks_of(a.variant) >= cus / 2) --a.variant;
+    const int bk = tile_keys(a.variant, f32);
+    const long long blocks = blocks_of(a.variant);
+    a.row_blocks = static_cast<int>(blocks / BH);
+    // few blocks of rows: their keys are split until every compute unit has work
     long long keys = a.N;
     if (a.score.window > 0) keys = keys < 2ll * a.score.window + a.T ? keys : 2ll * a.score.window + a.T;
     const long long tiles = (keys + bk - 1) / bk;
-    long long splits = blocks >= cus ? 1 : (2 * cus + blocks - 1) / blocks;
-    if (splits > tiles / 2) splits = tiles / 2;
+    long long splits = blocks >= cus ? 1 : per_cu(a.variant, a.d, f32, 1) * cus / blocks;
+    if (splits > tiles) splits = tiles;
     a.part.splits = static_cast<int>(splits < 1 ? 1 : splits > 128 ? 128 : splits);
     size_t at = 0;
     if (a.documents) {
