@@ -6,12 +6,15 @@
 
 namespace santapp {
 
-// Joins the split parts of one row, a workgroup per row: threads take a part's
-// maximum and sum each, then D / 4 lanes (four dims each) the values of every
-// kGroups-th part, several in flight.  The parts come in up to two runs
-// (prompt, suffix) of at most kMaxParts in all.
+// Joins the split parts of rows.  The parts of a row come in up to two runs
+// (prompt, suffix) of at most kMaxParts in all.  Rows of more than kFewParts take a
+// workgroup each: threads take a part's maximum and sum each, then D / 4 lanes
+// (four dims each) the values of every kGroups-th part, several in flight (99 us
+// with a lane walking all 128 parts of a row, 8 this way).  Otherwise D / 4 lanes
+// take a row (14336 rows of two parts: 35 us with a workgroup each, 15 this way).
 constexpr int kJoinThreads = 256;
 constexpr int kMaxParts = 320;
+constexpr int kFewParts = 8;
 
 struct JoinRun {
     const float2* ml;  // part i: ml[i stride], values o[i stride d]
@@ -36,8 +39,50 @@ __device__ __forceinline__ void store4(bf16_t* p, float4 v, float f) {
 // 1 / l, 0 for a row that attended nothing.
 __device__ __forceinline__ float inverse_sum(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
+template <int D>
+constexpr int join_rows(int parts) {
+    return parts <= kFewParts ? kJoinThreads / (D / 4) : 1;
+}
+
+// One row by D / 4 lanes.
 template <int D, typename TO>
-__device__ __forceinline__ void join_parts(const JoinRun (&runs)[2], TO* out) {
+__device__ __forceinline__ void join_few(const JoinRun (&runs)[2], TO* out) {
+    const int c = threadIdx.x % (D / 4), n = runs[0].n + runs[1].n;
+    float2 ml[kFewParts];
+    float4 y[kFewParts];
+#pragma unroll
+    for (int i = 0; i < kFewParts; ++i) {
+        ml[i] = make_float2(kNegInf, 0.f);
+        y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i < n) {
+            const int x = i < runs[0].n ? 0 : 1;
+            const long long at = (i - (x ? runs[0].n : 0)) * runs[x].stride;
+            ml[i] = runs[x].ml[at];
+            y[i] = reinterpret_cast<const float4*>(runs[x].o + at * D)[c];
+        }
+    }
+    float m = kNegInf, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < kFewParts; ++i)
+        if (ml[i].y != 0.f) m = fmaxf(m, ml[i].x);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kFewParts; ++i) {
+        const float f = ml[i].y == 0.f ? 0.f : exp2_fast(ml[i].x - m);
+        if (f != 0.f) {  // a part of no weight may hold anything
+            l = fmaf(f, ml[i].y, l);
+            v.x = fmaf(f, y[i].x, v.x);
+            v.y = fmaf(f, y[i].y, v.y);
+            v.z = fmaf(f, y[i].z, v.z);
+            v.w = fmaf(f, y[i].w, v.w);
+        }
+    }
+    store4(out + 4 * c, v, inverse_sum(l));
+}
+
+// One row by the workgroup.
+template <int D, typename TO>
+__device__ __forceinline__ void join_many(const JoinRun (&runs)[2], TO* out) {
     constexpr int L = D / 4, kGroups = kJoinThreads / L, kW = kJoinThreads / kWave;
     constexpr int kEach = (kMaxParts + kJoinThreads - 1) / kJoinThreads;
     __shared__ float s_w[kMaxParts];
@@ -133,7 +178,7 @@ inline size_t place_parts(PartArgs& p, long long pairs, long long rows, int d, c
 }
 
 // Row blocks by the rows of a pair: few rows spread the waves over keys.
-// Variant v is WR x WK of row_waves(v) x key_waves(v, dtype).
+// Variant v is WR x WK of row_waves(v) x key_waves(v, dtype), 32 WR rows a block.
 constexpr int variant_of(long long rows) { return rows <= 32 ? 0 : rows <= 64 ? 1 : 2; }
 constexpr int row_waves(int v) { return v == 0 ? 1 : v == 1 ? 2 : 4; }
 // fp32 tiles are twice as large: two waves over keys fill the LDS

@@ -122,13 +122,19 @@ __global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) 
 
 template <int D>
 __global__ __launch_bounds__(kJoinThreads) void k_prefix_join(PrefixArgs a) {
-    const int Hq = a.Hkv * a.G, row = blockIdx.x, b = row / Hq, h = row - b * Hq, kv = h / a.G, g = h - kv * a.G;
+    const int Hq = a.Hkv * a.G, per = join_rows<D>(a.part.splits + a.spart.splits);
+    const int row = blockIdx.x * per + (per > 1 ? threadIdx.x / (D / 4) : 0);
+    if (row >= a.P * a.S * Hq) return;
+    const int b = row / Hq, h = row - b * Hq, kv = h / a.G, g = h - kv * a.G;
     const int p = b / a.S, R = a.S * a.G;
     const long long f0 = (static_cast<long long>(p) * a.Hkv + kv) * a.part.splits * R + (b - p * a.S) * a.G + g;
     const long long f1 = (static_cast<long long>(b) * a.Hkv + kv) * a.spart.splits * a.G + g;
     const JoinRun runs[2] = {{a.part.ml + f0, a.part.o + f0 * D, R, a.part.splits},
                              {a.spart.ml + f1, a.spart.o + f1 * D, a.G, a.spart.splits}};
-    join_parts<D>(runs, a.out + static_cast<long long>(row) * D);
+    if (per > 1)  // uniform
+        join_few<D>(runs, a.out + static_cast<long long>(row) * D);
+    else
+        join_many<D>(runs, a.out + static_cast<long long>(row) * D);
 }
 
 template <typename T, int D>
@@ -152,7 +158,8 @@ hipError_t launch(const PrefixArgs& a, hipStream_t s) {
         run(std::integral_constant<int, 2>{});
     if (hipError_t e = hipGetLastError()) return e;
     if (a.part.splits + a.spart.splits > 1) {
-        k_prefix_join<D><<<dim3(static_cast<unsigned>(a.P * a.S * a.Hkv * a.G)), kJoinThreads, 0, s>>>(a);
+        const int per = join_rows<D>(a.part.splits + a.spart.splits);
+        k_prefix_join<D><<<dim3(static_cast<unsigned>((a.P * a.S * a.Hkv * a.G + per - 1) / per)), kJoinThreads, 0, s>>>(a);
     }
     return hipGetLastError();
 }

@@ -82,12 +82,18 @@ __global__ __launch_bounds__(64 * WR * WK, (Shape<T, D, 1, WR, WK>::kPerCu)) voi
 
 template <typename T, int D>
 __global__ __launch_bounds__(kJoinThreads) void k_prompt_join(PromptArgs a) {
-    const int R = a.T * a.G, pair = blockIdx.x / R, r = blockIdx.x - pair * R;
+    const int R = a.T * a.G, per = join_rows<D>(a.part.splits);
+    const long long row = static_cast<long long>(blockIdx.x) * per + (per > 1 ? threadIdx.x / (D / 4) : 0);
+    if (row >= static_cast<long long>(a.B) * a.Hkv * R) return;
+    const int pair = static_cast<int>(row / R), r = static_cast<int>(row - static_cast<long long>(pair) * R);
     const long long first = static_cast<long long>(pair) * a.part.splits * R + r;
     const JoinRun runs[2] = {{a.part.ml + first, a.part.o + first * D, R, a.part.splits}, {nullptr, nullptr, 0, 0}};
     const int b = pair / a.Hkv, kv = pair - b * a.Hkv, t = r / a.G, h = kv * a.G + r - t * a.G;
     char* p = const_cast<char*>(a.out.p) + b * a.out.b + h * a.out.h + t * a.out.t;
-    join_parts<D>(runs, reinterpret_cast<T*>(p));
+    if (per > 1)  // uniform
+        join_few<D>(runs, reinterpret_cast<T*>(p));
+    else
+        join_many<D>(runs, reinterpret_cast<T*>(p));
 }
 
 template <typename T, int D>
@@ -121,7 +127,8 @@ hipError_t launch(const PromptArgs& a, hipStream_t s) {
         modes(std::integral_constant<int, 2>{});
     if (hipError_t e = hipGetLastError()) return e;
     if (a.part.splits > 1) {
-        k_prompt_join<T, D><<<dim3(static_cast<unsigned>(BH * R)), kJoinThreads, 0, s>>>(a);
+        const int per = join_rows<D>(a.part.splits);
+        k_prompt_join<T, D><<<dim3(static_cast<unsigned>((BH * R + per - 1) / per)), kJoinThreads, 0, s>>>(a);
     }
     return hipGetLastError();
 }
@@ -132,21 +139,31 @@ size_t plan_prompt(PromptArgs& a, int cus, char* ws) {
     if (cus <= 0) cus = 256;
     const bool f32 = a.dtype == SANTAPP_FP32;
     const long long R = static_cast<long long>(a.T) * a.G, BH = static_cast<long long>(a.B) * a.Hkv;
-    a.variant = variant_of(R);
-    // blocks differ in length under a mask: of fewer than four per compute unit
-    // the longest set the time, so smaller ones are taken
+    // Blocks of 128 rows keep the matrix cores busiest, but under a mask they
+    // differ in length and the longest of few set the time, and blocks of 64 hide
+    // more of their start.  Causal prompts of 28 query and 4 KV heads of 128, bf16:
+    // 2048 tokens 62 us with 448 blocks of 128, 55 with 896 of 64; 4096 tokens
+    // 139 and 165.  fp32 (2048 tokens): 354 and 321; 16 heads of 64, 1009 tokens of
+    // two sequences: 79, 60, and 54 with 1024 blocks of 32.
     auto blocks_of = [&](int v) { return BH * ((R + 32 * row_waves(v) - 1) / (32 * row_waves(v))); };
-    while (a.variant > 0 && blocks_of(a.variant) < 4ll * cus && blocks_of(a.variant) >= cus / 2) --a.variant;
+    a.variant = variant_of(R);
+    if (a.variant == 2 && blocks_of(2) < (f32 ? 8ll : 3ll) * cus) a.variant = 1;
+    if (a.variant == 1 && f32 && a.d == 64 && blocks_of(1) >= cus && blocks_of(1) <= 2ll * cus) a.variant = 0;
     const int bk = tile_keys(a.variant, f32);
     const long long blocks = blocks_of(a.variant);
     a.row_blocks = static_cast<int>(blocks / BH);
-    // few blocks of rows: their keys are split until every compute unit has work
+    // Few blocks: their keys are split until every workgroup slot has work, but
+    // into parts long enough to pay for their join (rows x parts x d values): 128
+    // keys where rows are few, 512 otherwise, and 64 parts at most (5 of 32768
+    // tokens: 26 us with 128, 23 with 64; 256 of 8192 tokens: 114 us with one part,
+    // 59 with four)
     long long keys = a.N;
     if (a.score.window > 0) keys = keys < 2ll * a.score.window + a.T ? keys : 2ll * a.score.window + a.T;
-    const long long tiles = (keys + bk - 1) / bk;
-    long long splits = blocks >= cus ? 1 : per_cu(a.variant, a.d, f32, 1) * cus / blocks;
-    if (splits > tiles) splits = tiles;
-    a.part.splits = static_cast<int>(splits < 1 ? 1 : splits > 128 ? 128 : splits);
+    long long splits = per_cu(a.variant, a.d, f32, 1) * static_cast<long long>(cus) / blocks;
+    const long long most = keys / (R <= 64 ? 128 : 512), tiles = (keys + bk - 1) / bk;
+    splits = splits > most ? most : splits;
+    splits = splits > tiles ? tiles : splits;
+    a.part.splits = static_cast<int>(splits < 1 ? 1 : splits > 64 ? 64 : splits);
     size_t at = 0;
     if (a.documents) {
         a.doc_range = reinterpret_cast<int2*>(ws);
