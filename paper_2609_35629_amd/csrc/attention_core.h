@@ -46,7 +46,6 @@ struct KeySeg {
 struct RowInfo {
     int lo, hi, pos, doc;
     float slope;
-    bool valid;
 };
 
 // A lane's offset within a group of at most 32 rows has 32 bits.
@@ -157,18 +156,25 @@ struct Ops<bf16_t, D, NT> {
             x -= static_cast<float>(h);
         }
     }
-    __device__ __forceinline__ f32x16 scores(const char* ktile, int row0, int lane) const {
-        f32x16 s;
+    // Of KS x 32 keys, their products in turn.
+    template <int KS>
+    __device__ __forceinline__ void scores(const char* ktile, int row0, int lane, f32x16 (&s)[KS]) const {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        for (int u = 0; u < KS; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
         const int row = row0 + (lane & 31), hh = lane >> 5;
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-            const bf16x8 a = *reinterpret_cast<const bf16x8*>(ktile + TL::at(row, 16 * (2 * k + hh)));
+            bf16x8 a[KS];
 #pragma unroll
-            for (int t = NT - 1; t >= 0; --t) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[t][k], s, 0, 0, 0);
+            for (int u = 0; u < KS; ++u)
+                a[u] = *reinterpret_cast<const bf16x8*>(ktile + TL::at(row + 32 * u, 16 * (2 * k + hh)));
+#pragma unroll
+            for (int t = NT - 1; t >= 0; --t)
+#pragma unroll
+                for (int u = 0; u < KS; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[u], q[t][k], s[u], 0, 0, 0);
         }
-        return s;
     }
     // V^T of 4 keys x 16 dims per 16 lanes: lane s % 16 addresses key s / 4,
     // dims 4 (s % 4) .. + 4, lane n receives the four keys of dim n.
@@ -197,13 +203,14 @@ struct Ops<bf16_t, D, NT> {
                     x -= static_cast<float>(h);
                 }
             }
+            bf16x8 a[D / 32];
 #pragma unroll
-            for (int db = 0; db < D / 32; ++db) {
-                const bf16x8 a = values(vtile, row0 + 16 * k, db, lane);
+            for (int db = 0; db < D / 32; ++db) a[db] = values(vtile, row0 + 16 * k, db, lane);
 #pragma unroll
-                for (int t = NT - 1; t >= 0; --t)
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b[t], o[db], 0, 0, 0);
-            }
+            for (int t = NT - 1; t >= 0; --t)
+#pragma unroll
+                for (int db = 0; db < D / 32; ++db)
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[db], b[t], o[db], 0, 0, 0);
         }
     }
 };
@@ -219,7 +226,9 @@ struct Ops<float, D, 1> {
         for (int c = 0; c < D / 8; ++c) q[c] = *reinterpret_cast<const float4*>(row + 4 * (8 * c + 4 * hh));
     }
     __device__ __forceinline__ void ready() {}
-    __device__ __forceinline__ f32x16 scores(const char* ktile, int row0, int lane) const {
+    template <int KS>
+    __device__ __forceinline__ void scores(const char* ktile, int row0, int lane, f32x16 (&out)[KS]) const {
+        static_assert(KS == 1, "one stretch of fp32 keys at a time");
         f32x16 s;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
@@ -232,7 +241,7 @@ struct Ops<float, D, 1> {
             s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, q[c].z, s, 0, 0, 0);
             s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, q[c].w, s, 0, 0, 0);
         }
-        return s;
+        out[0] = s;
     }
     static __device__ __forceinline__ void add_values(const char* vtile, int row0, const f32x16& p, f32x16 (&o)[D / 32],
                                                       int lane) {
@@ -342,8 +351,9 @@ constexpr int kExtra = 1;  // a cap, or a bias by distance
 constexpr int kDocs = 2;   // documents
 
 // Attention of one block of rows over tiles of a stretch of keys.
-//   rowinfo(r)   RowInfo of the block's row r < BM
-//   qrow(r)      its query row (only of valid rows)
+//   rows         rows of the block, 1 .. BM
+//   rowinfo(r)   RowInfo of the block's row r < rows
+//   qrow(r)      its query row
 //   docs         (with kDocs) document of each key; ranges: lowest and highest
 //                of every kDocTile keys
 //   split/splits the part of the block's key tiles to walk
@@ -351,7 +361,7 @@ constexpr int kDocs = 2;   // documents
 // buf0, buf1: Shape::kBuf bytes of LDS each.
 template <typename T, int D, int NT, int WR, int WK, int MODE, bool EXACT, typename Info, typename QRow, typename Emit>
 __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, const int* docs, const int2* ranges,
-                                       int split, int splits, char* buf0, char* buf1, Info&& rowinfo, QRow&& qrow,
+                                       int split, int splits, char* buf0, char* buf1, int rows, Info&& rowinfo, QRow&& qrow,
                                        Emit&& emit) {
     using SH = Shape<T, D, NT, WR, WK>;
     using TL = Tile<T, D>;
@@ -366,15 +376,14 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
     int blo = seg.n, bhi = 0, dlo = 0x7fffffff, dhi = -0x7fffffff - 1;
 #pragma unroll
     for (int r = lane; r < SH::BM; r += kWave) {
+        if (r >= rows) break;
         const RowInfo x = rowinfo(r);
-        if (x.valid && x.lo < x.hi) {
+        if (x.lo < x.hi) {
             blo = min(blo, x.lo);
             bhi = max(bhi, x.hi);
         }
-        if (x.valid) {
-            dlo = min(dlo, x.doc);
-            dhi = max(dhi, x.doc);
-        }
+        dlo = min(dlo, x.doc);
+        dhi = max(dhi, x.doc);
     }
     blo = wave_min_i32(blo);
     bhi = wave_max_i32(bhi);
@@ -382,7 +391,8 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
         dlo = wave_min_i32(dlo);
         dhi = wave_max_i32(dhi);
     }
-    RowInfo me = rowinfo(32 * wr + (lane & 31));
+    const bool mine = 32 * wr + (lane & 31) < rows;  // whether the lane's row is one
+    RowInfo me = rowinfo(mine ? 32 * wr + (lane & 31) : 0);
     // Rows of one document whose keys are one run [lo, hi) (packed documents)
     // attend within the run; documents are compared key by key otherwise.
     bool by_key = false;
@@ -398,10 +408,10 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
         }
     }
     // keys that every row of the wave may attend, and that any may
-    const int wlo = wave_max_i32(me.valid ? me.lo : 0), whi = wave_min_i32(me.valid ? me.hi : seg.n);
-    const int vlo = wave_min_i32(me.valid ? me.lo : seg.n), vhi = wave_max_i32(me.valid ? me.hi : 0);
+    const int wlo = wave_max_i32(mine ? me.lo : 0), whi = wave_min_i32(mine ? me.hi : seg.n);
+    const int vlo = wave_min_i32(mine ? me.lo : seg.n), vhi = wave_max_i32(mine ? me.hi : 0);
 
-    const int wpos = wave_min_i32(me.valid ? me.pos : 0x7fffffff);  // the foremost query
+    const int wpos = wave_min_i32(mine ? me.pos : 0x7fffffff);  // the foremost query
 
     // this split's tiles
     int t0 = blo / BK, t1 = bhi > blo ? (bhi + BK - 1) / BK : t0;
@@ -485,7 +495,7 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
     };
 
     OP op;
-    op.load_q(qrow(me.valid ? 32 * wr + (lane & 31) : 0), hh);
+    op.load_q(qrow(mine ? 32 * wr + (lane & 31) : 0), hh);
     float m, l;
     f32x16 o[D / 32];
 
@@ -502,8 +512,7 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
         const int k0 = t * BK + in_tile;
         if (k0 >= vhi || k0 + 32 * KS <= vlo) return;
         f32x16 s[KS];
-#pragma unroll
-        for (int u = 0; u < KS; ++u) s[u] = op.scores(buf, in_tile + 32 * u, lane);
+        op.scores(buf, in_tile, lane, s);
         __builtin_amdgcn_s_setprio(0);
         if constexpr (EXTRA) {
             // s = scale q.k, capped, less the slope times the distance; with no
@@ -661,13 +670,17 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
             alone = (same >> (t - seen)) & 1;
         }
     };
+    __shared__ int s_special;
+    if (threadIdx.x == 0) s_special = 0;  // before the first tile's barrier; without tiles no value is special
     walk(std::false_type{});
     float z = 0.f;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) z = fmaf(o[db][i], 0.f, z);
-    if (__syncthreads_or(me.valid && z != 0.f)) {
+    if (__any(mine && z != 0.f) && lane == 0) s_special = 1;
+    __syncthreads();
+    if (s_special) {  // uniform
         uint32_t has[3][D / 64];  // +infinity, -infinity, NaN of value 16 db + i
 #pragma unroll 1
         for (pass = 4; pass > 0; --pass) {
@@ -700,7 +713,7 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
     l = add_halves(l);
 
     if constexpr (WK == 1) {
-        if (me.valid) {
+        if (mine) {
 #pragma unroll
             for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -730,7 +743,7 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
         __syncthreads();
         for (int x = threadIdx.x; x < SH::BM * (D / 4); x += NW * kWave) {
             const int r = x / (D / 4), dim = 4 * (x % (D / 4));
-            if (!rowinfo(r).valid) continue;
+            if (r >= rows) continue;
             float mm = kNegInf;
 #pragma unroll
             for (int k = 0; k < WK; ++k) mm = fmaxf(mm, state(k * WR + r / 32)[(r % 32) * ST + D]);

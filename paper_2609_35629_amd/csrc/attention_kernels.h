@@ -8,10 +8,9 @@ namespace santapp {
 
 // Joins the split parts of rows.  The parts of a row come in up to two runs
 // (prompt, suffix) of at most kMaxParts in all.  Rows of more than kFewParts take a
-// workgroup each: threads take a part's maximum and sum each, then D / 4 lanes
-// (four dims each) the values of every kGroups-th part, several in flight (99 us
-// with a lane walking all 128 parts of a row, 8 this way).  Otherwise D / 4 lanes
-// take a row (14336 rows of two parts: 35 us with a workgroup each, 15 this way).
+// workgroup each, several parts in flight (140 rows of 128 parts: 99 us with a
+// lane walking all parts of a row, 8 with a workgroup).  Otherwise D / 4 lanes
+// take a row (14336 rows of two parts: 20 us with a workgroup each, 5 this way).
 constexpr int kJoinThreads = 256;
 constexpr int kMaxParts = 320;
 constexpr int kFewParts = 8;
@@ -80,62 +79,74 @@ __device__ __forceinline__ void join_few(const JoinRun (&runs)[2], TO* out) {
     store4(out + 4 * c, v, inverse_sum(l));
 }
 
-// One row by the workgroup.
+// One row by the workgroup: every wave finds the maximum and the weights of all
+// parts for itself (part i in lane i % 64), while the first values are on their
+// way; D / 4 lanes take the values of every kGroups-th part.
 template <int D, typename TO>
 __device__ __forceinline__ void join_many(const JoinRun (&runs)[2], TO* out) {
-    constexpr int L = D / 4, kGroups = kJoinThreads / L, kW = kJoinThreads / kWave;
-    constexpr int kEach = (kMaxParts + kJoinThreads - 1) / kJoinThreads;
-    __shared__ float s_w[kMaxParts];
-    __shared__ float s_red[2 * kW];
+    constexpr int L = D / 4, kGroups = kJoinThreads / L;
+    constexpr int kEach = kMaxParts / kWave, kChunk = kWave / kGroups;  // parts of a lane; of a group per 64
+    static_assert(kEach * kWave == kMaxParts && kChunk * kGroups == kWave, "whole chunks");
     __shared__ float4 s_v[kGroups][L];
-    const int n = runs[0].n + runs[1].n;
-    auto of = [&](int i, const float*& o) {
-        const int x = i < runs[0].n ? 0 : 1;
-        const long long at = (i - (x ? runs[0].n : 0)) * runs[x].stride;
-        o = runs[x].o + at * D;
-        return runs[x].ml + at;
+    const int n = runs[0].n + runs[1].n, lane = lane_id();
+    const int g = threadIdx.x / L, c = threadIdx.x % L;
+    auto place = [&](int i, int& x) {
+        x = i < runs[0].n ? 0 : 1;
+        return (i - (x ? runs[0].n : 0)) * runs[x].stride;
     };
-    const float* unused;
     float2 ml[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int i = lane + kWave * k;
+        ml[k] = make_float2(kNegInf, 0.f);
+        if (i < n) {
+            int x;
+            const long long at = place(i, x);
+            ml[k] = runs[x].ml[at];
+        }
+    }
+    float4 y[kChunk];
+    auto load = [&](int k) {
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) {
+            const int i = kWave * k + kGroups * j + g;
+            y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (i < n) {
+                int x;
+                const long long at = place(i, x);
+                y[j] = reinterpret_cast<const float4*>(runs[x].o + at * D)[c];
+            }
+        }
+    };
+    load(0);
     float m = kNegInf, l = 0.f;
 #pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-        const int i = threadIdx.x + k * kJoinThreads;
-        ml[k] = i < n ? *of(i, unused) : make_float2(kNegInf, 0.f);
+    for (int k = 0; k < kEach; ++k)
         if (ml[k].y != 0.f) m = fmaxf(m, ml[k].x);
-    }
     m = wave_max_f32(m);
-    if (lane_id() == 0) s_red[wave_id()] = m;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kW; ++w) m = fmaxf(m, s_red[w]);
+    float w[kEach];
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
-        const int i = threadIdx.x + k * kJoinThreads;
-        const float f = ml[k].y == 0.f ? 0.f : exp2_fast(ml[k].x - m);  // nothing attended: 0
-        if (i < n) s_w[i] = f;
-        l += f == 0.f ? 0.f : f * ml[k].y;
+        w[k] = ml[k].y == 0.f ? 0.f : exp2_fast(ml[k].x - m);  // nothing attended: 0
+        if (w[k] != 0.f) l = fmaf(w[k], ml[k].y, l);
     }
-#pragma unroll
-    for (int k = 1; k < kWave; k *= 2) l += __shfl_xor(l, k);
-    if (lane_id() == 0) s_red[kW + wave_id()] = l;
-    __syncthreads();
-    l = 0.f;
-#pragma unroll
-    for (int w = 0; w < kW; ++w) l += s_red[kW + w];
-    const int g = threadIdx.x / L, c = threadIdx.x % L;
+    l = row16_sum(l);
+    l = add_halves(l);
+    l += __shfl_xor(l, 16);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int i = g; i < n; i += kGroups) {
-        const float* o;
-        of(i, o);
-        const float f = s_w[i];
-        const float4 y = reinterpret_cast<const float4*>(o)[c];
-        if (f != 0.f) {  // a part of no weight may hold anything
-            v.x = fmaf(f, y.x, v.x);
-            v.y = fmaf(f, y.y, v.y);
-            v.z = fmaf(f, y.z, v.z);
-            v.w = fmaf(f, y.w, v.w);
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        if (kWave * k >= n) break;  // uniform
+        if (k > 0) load(k);
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) {
+            const float f = __shfl(w[k], kGroups * j + g);
+            if (f != 0.f) {  // a part of no weight may hold anything
+                v.x = fmaf(f, y[j].x, v.x);
+                v.y = fmaf(f, y[j].y, v.y);
+                v.z = fmaf(f, y[j].z, v.z);
+                v.w = fmaf(f, y[j].w, v.w);
+            }
         }
     }
     s_v[g][c] = v;
@@ -144,11 +155,11 @@ __device__ __forceinline__ void join_many(const JoinRun (&runs)[2], TO* out) {
         v = s_v[0][c];
 #pragma unroll
         for (int k = 1; k < kGroups; ++k) {
-            const float4 y = s_v[k][c];
-            v.x += y.x;
-            v.y += y.y;
-            v.z += y.z;
-            v.w += y.w;
+            const float4 z = s_v[k][c];
+            v.x += z.x;
+            v.y += z.y;
+            v.z += z.z;
+            v.w += z.w;
         }
         store4(out + 4 * c, v, inverse_sum(l));
     }

@@ -1,6 +1,8 @@
 // Decoding of several sequences over a prompt they share: each prompt's keys and
 // values are read once for all its sequences, each sequence's suffix rows once
 // for its heads, and the parts are joined.
+#include <algorithm>
+
 #include "attention_kernels.h"
 
 namespace santapp {
@@ -50,8 +52,7 @@ __global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) 
         seg.n = clamped(a.prefix_lengths, p, a.N);
         auto rowinfo = [&](int r) {
             RowInfo x;
-            x.valid = r0 + r < R;
-            const int row = min(r0 + r, R - 1), i = row / a.G, b = p * a.S + i, h = kv * a.G + row - i * a.G;
+            const int row = r0 + r, i = row / a.G, b = p * a.S + i, h = kv * a.G + row - i * a.G;
             const long long pos = a.positions ? static_cast<long long>(a.positions[b])
                                               : static_cast<long long>(seg.n) + clamped(a.lengths, b, a.T) - 1;
             x.pos = clamp_pos(pos);
@@ -76,7 +77,8 @@ __global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) 
             else
                 store4(a.out + head(r) * D + dim, v, inverse_sum(l));
         };
-        attend<T, D, NT, WR, WK, MODE, true>(seg, a.score, nullptr, nullptr, split, a.part.splits, buf0, buf1, rowinfo, qrow,
+        attend<T, D, NT, WR, WK, MODE, true>(seg, a.score, nullptr, nullptr, split, a.part.splits, buf0, buf1,
+                                              min(SH::BM, R - r0), rowinfo, qrow,
                                             emit);
         return;
     }
@@ -96,7 +98,6 @@ __global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) 
                                        : static_cast<long long>(seg.n) - 1);
     auto rowinfo = [&](int r) {
         RowInfo x;
-        x.valid = r0 + r < a.G;
         x.pos = clamp_pos(pos);
         x.lo = 0;
         x.hi = seg.n;
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) 
             x.hi = static_cast<int>(min(max(pos + a.score.window, 0ll), static_cast<long long>(seg.n)));
         }
         x.doc = 0;
-        x.slope = (MODE & kExtra) != 0 && a.score.slopes ? a.score.slopes[kv * a.G + min(r0 + r, a.G - 1)] * 1.44269504088896341f : 0.f;
+        x.slope = (MODE & kExtra) != 0 && a.score.slopes ? a.score.slopes[kv * a.G + r0 + r] * 1.44269504088896341f : 0.f;
         return x;
     };
     auto head = [&](int r) { return static_cast<long long>(b) * Hq + kv * a.G + r0 + r; };
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) 
             store4(a.out + head(r) * D + dim, v, inverse_sum(l));
     };
     attend<T, D, NT, WR * WK / SK, SK, MODE, true>(seg, a.score, nullptr, nullptr, split, a.spart.splits, buf0, buf1,
-                                                       rowinfo, qrow, emit);
+                                                         min(SS::BM, a.G - r0), rowinfo, qrow, emit);
 }
 
 template <int D>
@@ -170,7 +171,10 @@ size_t plan_prefix(PrefixArgs& a, int cus, char* ws) {
     if (cus <= 0) cus = 256;
     const bool f32 = a.dtype == SANTAPP_FP32;
     const long long R = static_cast<long long>(a.S) * a.G, pairs = static_cast<long long>(a.P) * a.Hkv;
+    // blocks of 64 rows where 128 would leave more of the last one empty (64
+    // sequences of 7 heads: 448 rows)
     a.variant = variant_of(R);
+    if (a.variant == 2 && (R + 63) / 64 * 64 < (R + 127) / 128 * 128) a.variant = 1;
     const int bm = 32 * row_waves(a.variant), bk = tile_keys(a.variant, f32);
     const long long slots = static_cast<long long>(per_cu(a.variant, a.d, f32, f32 ? 1 : 3)) * cus;
     // the suffixes: a block per 32 heads (times the waves over rows) each, split
@@ -186,17 +190,26 @@ size_t plan_prefix(PrefixArgs& a, int cus, char* ws) {
         k = k > tiles ? tiles : k;
         a.spart.splits = static_cast<int>(k < 1 ? 1 : k > 64 ? 64 : k);
     }
-    // the prompts: as many splits as leave every workgroup slot one block, the
-    // suffixes' included
+    // the prompts: the splits whose blocks, and the suffixes' in the slots left
+    // over, are done first; a block costs its tiles and about two tiles' time for
+    // its start and end (8 of about 4 us)
     a.row_blocks = a.N > 0 ? static_cast<int>((R + bm - 1) / bm) : 0;
     const long long blocks = pairs * a.row_blocks;
     a.part.splits = 0;
     if (blocks > 0) {
-        const long long tiles = (a.N + bk - 1) / bk;
-        const long long left = slots - sblocks * a.spart.splits;
-        long long k = (left > slots / 2 ? left : slots) / blocks;
-        if (k > tiles) k = tiles;
-        a.part.splits = static_cast<int>(k < 1 ? 1 : k > 256 ? 256 : k);
+        const long long tiles = (a.N + bk - 1) / bk, ns = sblocks * a.spart.splits;
+        const long long scost = 2 + (ns ? ((a.T + 32 * kw - 1) / (32 * kw) + a.spart.splits - 1) / a.spart.splits : 0);
+        long long best = -1;
+        const long long most = std::min<long long>(std::min<long long>(tiles, 256), std::max<long long>(1, 4 * slots / blocks));
+        for (long long k = 1; k <= most; ++k) {
+            const long long cost = 2 + (tiles + k - 1) / k, rounds = (blocks * k + slots - 1) / slots;
+            const long long idle = rounds * slots - blocks * k, more = ns > idle ? (ns - idle + slots - 1) / slots : 0;
+            const long long time = std::max(rounds * cost, (rounds - 1) * cost + scost) + more * scost;
+            if (best < 0 || time < best) {
+                best = time;
+                a.part.splits = static_cast<int>(k);
+            }
+        }
     }
     if (a.part.splits + a.spart.splits <= 1) return 0;
     size_t at = 0;

@@ -47,8 +47,7 @@ __global__ __launch_bounds__(64 * WR * WK, (Shape<T, D, 1, WR, WK>::kPerCu)) voi
     const int prefix = a.prefix ? a.prefix[b] : 0;
     auto rowinfo = [&](int r) {
         RowInfo x;
-        x.valid = r0 + r < R;
-        const int row = min(r0 + r, R - 1), t = row / a.G, h = kv * a.G + row - t * a.G;
+        const int row = r0 + r, t = row / a.G, h = kv * a.G + row - t * a.G;
         x.pos = a.offset + t;
         int lo = 0, hi = a.N;
         if (a.causal) hi = min(hi, max(x.pos + 1, prefix));
@@ -76,7 +75,8 @@ __global__ __launch_bounds__(64 * WR * WK, (Shape<T, D, 1, WR, WK>::kPerCu)) voi
         store4(reinterpret_cast<T*>(p) + dim, v, inverse_sum(l));
     };
     const int2* ranges = docs ? a.doc_range + static_cast<long long>(b) * ((a.N + kDocTile - 1) / kDocTile) : nullptr;
-    attend<T, D, 1, WR, WK, MODE, sizeof(T) == 4>(seg, a.score, docs, ranges, split, a.part.splits, buf0, buf1, rowinfo,
+    attend<T, D, 1, WR, WK, MODE, sizeof(T) == 4>(seg, a.score, docs, ranges, split, a.part.splits, buf0, buf1,
+                                                 min(SH::BM, R - r0), rowinfo,
                                                  qrow, emit);
 }
 
