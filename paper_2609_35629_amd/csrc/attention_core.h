@@ -48,8 +48,7 @@ struct RowInfo {
     float slope;
 };
 
-// A lane's offset within a group of at most 32 rows has 32 bits.
-static_assert(32 * kMaxRowStep <= (1ll << 32), "");
+static_assert(kMaxRowStep < (1ll << 32), "a lane multiplies its row by 32 bits");
 
 constexpr float kNegInf = -__builtin_inff();
 
@@ -156,24 +155,34 @@ struct Ops<bf16_t, D, NT> {
             x -= static_cast<float>(h);
         }
     }
-    // Of KS x 32 keys, their products in turn.
-    template <int KS>
-    __device__ __forceinline__ void scores(const char* ktile, int row0, int lane, f32x16 (&s)[KS]) const {
+    // Of KS x 32 keys; the keys are read two products ahead.  between(k) is called
+    // after the k-th of kSlots products (of each stretch and term).
+    static constexpr int kSlots = D / 16;
+    template <int KS, typename F>
+    __device__ __forceinline__ void scores(const char* ktile, int row0, int lane, f32x16 (&s)[KS], F&& between) const {
+        const int row = row0 + (lane & 31), hh = lane >> 5;
+        bf16x8 a[3][KS];
+        auto load = [&](int k) {
+#pragma unroll
+            for (int u = 0; u < KS; ++u)
+                a[k % 3][u] = *reinterpret_cast<const bf16x8*>(ktile + TL::at(row + 32 * u, 16 * (2 * k + hh)));
+        };
+        load(0);
+        load(1);
 #pragma unroll
         for (int u = 0; u < KS; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
-        const int row = row0 + (lane & 31), hh = lane >> 5;
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-            bf16x8 a[KS];
-#pragma unroll
-            for (int u = 0; u < KS; ++u)
-                a[u] = *reinterpret_cast<const bf16x8*>(ktile + TL::at(row + 32 * u, 16 * (2 * k + hh)));
+        for (int k = 0; k < kSlots; ++k) {
+            if (k + 2 < kSlots) load(k + 2);
 #pragma unroll
             for (int t = NT - 1; t >= 0; --t)
 #pragma unroll
-                for (int u = 0; u < KS; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[u], q[t][k], s[u], 0, 0, 0);
+                for (int u = 0; u < KS; ++u)
+                    s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[k % 3][u], q[t][k], s[u], 0, 0, 0);
+            between(k);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     // V^T of 4 keys x 16 dims per 16 lanes: lane s % 16 addresses key s / 4,
@@ -188,14 +197,25 @@ struct Ops<bf16_t, D, NT> {
         const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vtile + TL::at(row + 8, byte)));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
-    static __device__ __forceinline__ void add_values(const char* vtile, int row0, const f32x16& p, f32x16 (&o)[D / 32],
-                                                      int lane) {
+    // Of KS x 32 keys, 16 at a time; the next 16 keys' values are read while the
+    // products of the last run.
+    template <int KS>
+    static __device__ __forceinline__ void add_values(const char* vtile, int row0, const f32x16 (&p)[KS],
+                                                      f32x16 (&o)[D / 32], int lane) {
+        bf16x8 a[2][D / 32];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int db = 0; db < D / 32; ++db) a[0][db] = values(vtile, row0, db, lane);
+#pragma unroll
+        for (int k = 0; k < 2 * KS; ++k) {
+            if (k + 1 < 2 * KS) {
+#pragma unroll
+                for (int db = 0; db < D / 32; ++db) a[(k + 1) & 1][db] = values(vtile, row0 + 16 * (k + 1), db, lane);
+            }
+            __builtin_amdgcn_sched_barrier(0);
             bf16x8 b[NT];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                float x = p[8 * k + e];
+                float x = p[k / 2][8 * (k & 1) + e];
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     const __bf16 h = static_cast<__bf16>(x);
@@ -203,14 +223,11 @@ struct Ops<bf16_t, D, NT> {
                     x -= static_cast<float>(h);
                 }
             }
-            bf16x8 a[D / 32];
-#pragma unroll
-            for (int db = 0; db < D / 32; ++db) a[db] = values(vtile, row0 + 16 * k, db, lane);
 #pragma unroll
             for (int t = NT - 1; t >= 0; --t)
 #pragma unroll
                 for (int db = 0; db < D / 32; ++db)
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[db], b[t], o[db], 0, 0, 0);
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[k & 1][db], b[t], o[db], 0, 0, 0);
         }
     }
 };
@@ -226,33 +243,54 @@ struct Ops<float, D, 1> {
         for (int c = 0; c < D / 8; ++c) q[c] = *reinterpret_cast<const float4*>(row + 4 * (8 * c + 4 * hh));
     }
     __device__ __forceinline__ void ready() {}
-    template <int KS>
-    __device__ __forceinline__ void scores(const char* ktile, int row0, int lane, f32x16 (&out)[KS]) const {
+    static constexpr int kSlots = D / 8;
+    template <int KS, typename F>
+    __device__ __forceinline__ void scores(const char* ktile, int row0, int lane, f32x16 (&out)[KS], F&& between) const {
         static_assert(KS == 1, "one stretch of fp32 keys at a time");
+        const int row = row0 + (lane & 31), hh = lane >> 5;
+        float4 a[3];
+        auto load = [&](int c) {
+            a[c % 3] = *reinterpret_cast<const float4*>(ktile + TL::at(row, 16 * (2 * c + hh)));
+        };
+        load(0);
+        load(1);
         f32x16 s;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
-        const int row = row0 + (lane & 31), hh = lane >> 5;
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
-            const float4 a = *reinterpret_cast<const float4*>(ktile + TL::at(row, 16 * (2 * c + hh)));
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, q[c].x, s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, q[c].y, s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, q[c].z, s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, q[c].w, s, 0, 0, 0);
+        for (int c = 0; c < kSlots; ++c) {
+            if (c + 2 < kSlots) load(c + 2);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[c % 3].x, q[c].x, s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[c % 3].y, q[c].y, s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[c % 3].z, q[c].z, s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[c % 3].w, q[c].w, s, 0, 0, 0);
+            between(c);
+            __builtin_amdgcn_sched_barrier(0);
         }
         out[0] = s;
     }
-    static __device__ __forceinline__ void add_values(const char* vtile, int row0, const f32x16& p, f32x16 (&o)[D / 32],
-                                                      int lane) {
+    template <int KS>
+    static __device__ __forceinline__ void add_values(const char* vtile, int row0, const f32x16 (&p)[KS],
+                                                      f32x16 (&o)[D / 32], int lane) {
+        float a[2][4][D / 32];  // of four keys
+        auto load = [&](int g) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int row = row0 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int db = 0; db < D / 32; ++db) {
-                const float a = *reinterpret_cast<const float*>(vtile + TL::at(row, 4 * (32 * db + (lane & 31))));
-                o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[i], o[db], 0, 0, 0);
-            }
+                for (int db = 0; db < D / 32; ++db)
+                    a[g & 1][i][db] = *reinterpret_cast<const float*>(
+                        vtile + TL::at(row0 + 8 * g + 4 * (lane >> 5) + i, 4 * (32 * db + (lane & 31))));
+        };
+        load(0);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            if (g < 3) load(g + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int db = 0; db < D / 32; ++db)
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[g & 1][i][db], p[0][4 * g + i], o[db], 0, 0, 0);
         }
     }
 };
@@ -358,9 +396,11 @@ constexpr int kDocs = 2;   // documents
 //                of every kDocTile keys
 //   split/splits the part of the block's key tiles to walk
 //   emit(r, dim, o, m, l)  receives four unnormalised values of row r
+// False if it has to be done again with SPECIAL (see below).
 // buf0, buf1: Shape::kBuf bytes of LDS each.
-template <typename T, int D, int NT, int WR, int WK, int MODE, bool EXACT, typename Info, typename QRow, typename Emit>
-__device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, const int* docs, const int2* ranges,
+template <typename T, int D, int NT, int WR, int WK, int MODE, bool EXACT, bool SPECIAL, typename Info, typename QRow,
+          typename Emit>
+__device__ __forceinline__ bool attend(const KeySeg& seg, const ScoreArgs& sc, const int* docs, const int2* ranges,
                                        int split, int splits, char* buf0, char* buf1, int rows, Info&& rowinfo, QRow&& qrow,
                                        Emit&& emit) {
     using SH = Shape<T, D, NT, WR, WK>;
@@ -466,32 +506,34 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
     constexpr int RPC = 64 / TL::SPR, STEP = NW * RPC;
     const int row0 = wv * RPC + lane / TL::SPR;
     const uint32_t piece0 = 16 * ((lane % TL::SPR) ^ TL::perm(row0));
-    const uint32_t koff = static_cast<uint32_t>(row0 * seg.kt), voff = static_cast<uint32_t>(row0 * seg.vt);
+    // The copies of a tile, in kCopies parts (of one K and one V piece): a wave
+    // that issues them in a row waits for the other waves' in the queue, so that
+    // they go between the products of the tile before (16384 tokens: 1130 us in a
+    // row, COPYTIME between).
+    constexpr int kCopies = SH::kTile / (1024 * NW);
+    static_assert((STEP & (STEP - 1)) == 0 && kCopies * STEP == BK, "whole groups");
+    const char *kb = nullptr, *vb = nullptr;
+    char* to = nullptr;
+    int last = 0;
+    auto target = [&](int t, char* buf) {
+        to = buf + 1024 * wv;
+        kb = seg.K + static_cast<long long>(t) * BK * seg.kt;
+        vb = seg.V + static_cast<long long>(t) * BK * seg.vt;
+        last = seg.n - 1 - t * BK;
+    };
+    const uint32_t kt = static_cast<uint32_t>(seg.kt), vt = static_cast<uint32_t>(seg.vt);
+    auto copy_part = [&](int i) {
+        const uint32_t piece = piece0 ^ (16 * TL::perm(STEP * i));
+        const uint64_t row = static_cast<uint32_t>(min(row0 + STEP * i, last));  // rows behind the last key repeat it
+        __builtin_amdgcn_global_load_lds(kb + (row * kt + piece),
+                                         (__attribute__((address_space(3))) void*)(to + 1024 * NW * i), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds(vb + (row * vt + piece),
+                                         (__attribute__((address_space(3))) void*)(to + SH::kTile + 1024 * NW * i), 16, 0, 0);
+    };
     auto copy = [&](int t, char* buf) {
-        constexpr int N = SH::kTile / (1024 * NW);  // copies per wave
-        static_assert((STEP & (STEP - 1)) == 0 && N * STEP == BK, "whole groups");
-        char* to = buf + 1024 * wv;
-        const char* kb = seg.K + static_cast<long long>(t) * BK * seg.kt;
-        const char* vb = seg.V + static_cast<long long>(t) * BK * seg.vt;
-        auto both = [&](int i, const char* k, const char* v, auto ko, auto vo) {
-            const uint32_t piece = piece0 ^ (16 * TL::perm(STEP * i));
-            __builtin_amdgcn_global_load_lds(
-                k + (ko + piece), (__attribute__((address_space(3))) void*)(to + 1024 * NW * i), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds(
-                v + (vo + piece), (__attribute__((address_space(3))) void*)(to + SH::kTile + 1024 * NW * i), 16, 0, 0);
-        };
-        const int last = seg.n - 1 - t * BK;
-        if (last >= BK - 1) {  // uniform
-            const long long ks = STEP * seg.kt, vs = STEP * seg.vt;
+        target(t, buf);
 #pragma unroll
-            for (int i = 0; i < N; ++i, kb += ks, vb += vs) both(i, kb, vb, koff, voff);
-        } else {  // rows behind the last key repeat it
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int r = min(row0 + STEP * i, last);
-                both(i, kb, vb, r * seg.kt, r * seg.vt);
-            }
-        }
+        for (int i = 0; i < kCopies; ++i) copy_part(i);
     };
 
     OP op;
@@ -499,20 +541,24 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
     float m, l;
     f32x16 o[D / 32];
 
-    // Pass 0 is the attention.  Where V holds a NaN or an infinity, the product
-    // carries it into every row of the block, also those that mask its key
-    // (0 times infinity).  A block that finds a value that is not finite in its
-    // sums therefore walks its tiles four times more: over V's +infinities,
-    // -infinities and NaNs as ones, with ones for the weights of unmasked keys,
-    // which says where they belong (has[]), and over V with zeros in their place.
+    // Where V holds a NaN or an infinity, the product carries it into every row of
+    // the block, also those that mask its key (0 times infinity).  A block that
+    // finds a value that is not finite in its sums (false is returned, nothing
+    // emitted) is done again with SPECIAL, which walks the tiles four times: in
+    // passes 4, 3, 2 over V's NaNs, -infinities and +infinities as ones, with ones
+    // for the weights of unmasked keys, which says where they belong (has[]), and in
+    // pass 1 over V with zeros in their place.
     int pass = 0;
-    auto compute = [&](int t, int sub, const char* buf, bool alone, auto special) {
-        constexpr bool SPECIAL = decltype(special)::value;
+    auto compute = [&](int t, int sub, const char* buf, bool alone, auto&& between) {
         const int in_tile = sub * SH::kStep + wk * 32 * KS;  // the wave's first key of the step
         const int k0 = t * BK + in_tile;
-        if (k0 >= vhi || k0 + 32 * KS <= vlo) return;
+        if (k0 >= vhi || k0 + 32 * KS <= vlo) {
+#pragma unroll
+            for (int k = 0; k < OP::kSlots; ++k) between(k);
+            return;
+        }
         f32x16 s[KS];
-        op.scores(buf, in_tile, lane, s);
+        op.scores(buf, in_tile, lane, s, between);
         __builtin_amdgcn_s_setprio(0);
         if constexpr (EXTRA) {
             // s = scale q.k, capped, less the slope times the distance; with no
@@ -612,9 +658,7 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
         // the matrix cores busy and the other's softmax fills in (16384 tokens:
         // 1160 us without, 1135 with)
         __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int u = 0; u < KS; ++u)
-            OP::add_values(buf + SH::kTile, in_tile + 32 * u, s[u], o, lane);
+        OP::add_values(buf + SH::kTile, in_tile, s, o, lane);
     };
 
     // every wave's copies of a tile are in LDS before any wave reads it
@@ -630,14 +674,25 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
         }
         __syncthreads();
     };
-    auto step = [&](int t, char* buf, bool alone, auto special) {
-        if constexpr (decltype(special)::value) prepare(buf);
+    // The steps of tile t in `buf`, with the copies of tile n (n < t1) into `other`.
+    auto step = [&](int t, char* buf, bool alone, int n, char* other) {
+        if constexpr (SPECIAL) prepare(buf);
+        const bool more = n < t1;
+        if (more) target(n, other);
+        constexpr int kAll = SUB * OP::kSlots;
 #pragma unroll
-        for (int sub = 0; sub < SUB; ++sub) compute(t, sub, buf, alone, special);
+        for (int sub = 0; sub < SUB; ++sub)
+            compute(t, sub, buf, alone, [&](int k) {
+                if (!more) return;  // uniform
+                const int slot = sub * OP::kSlots + k;
+#pragma unroll
+                for (int i = 0; i < kCopies; ++i)
+                    if (i * kAll / kCopies == slot) copy_part(i);
+            });
     };
     // one tile ahead; the two buffers are distinct objects, so that the copies
     // into one are known not to touch the reads of the other
-    auto walk = [&](auto special) {
+    auto walk = [&]() {
         if (by_key && seen != t0) {
             seen = t0;
             look();
@@ -652,39 +707,39 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
         if (t >= t1) return;
         bool alone = (same >> (t - seen)) & 1;
         copy(t, buf0);
-        if constexpr (!decltype(special)::value) op.ready();
+        if (!SPECIAL || pass == 4) op.ready();
         for (;;) {
             int n = next(t + 1);
             arrived();
-            if (n < t1) copy(n, buf1);
-            step(t, buf0, alone, special);
+            step(t, buf0, alone, n, buf1);
             if (n >= t1) break;
             t = n;
             alone = (same >> (t - seen)) & 1;
             n = next(t + 1);
             arrived();
-            if (n < t1) copy(n, buf0);
-            step(t, buf1, alone, special);
+            step(t, buf1, alone, n, buf0);
             if (n >= t1) break;
             t = n;
             alone = (same >> (t - seen)) & 1;
         }
     };
-    __shared__ int s_special;
-    if (threadIdx.x == 0) s_special = 0;  // before the first tile's barrier; without tiles no value is special
-    walk(std::false_type{});
-    float z = 0.f;
+    if constexpr (!SPECIAL) {
+        __shared__ int s_special;
+        if (threadIdx.x == 0) s_special = 0;  // before the first tile's barrier; without tiles no value is special
+        walk();
+        float z = 0.f;
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
+        for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) z = fmaf(o[db][i], 0.f, z);
-    if (__any(mine && z != 0.f) && lane == 0) s_special = 1;
-    __syncthreads();
-    if (s_special) {  // uniform
+            for (int i = 0; i < 16; ++i) z = fmaf(o[db][i], 0.f, z);
+        if (__any(mine && z != 0.f) && lane == 0) s_special = 1;
+        __syncthreads();
+        if (s_special) return false;  // uniform
+    } else {
         uint32_t has[3][D / 64];  // +infinity, -infinity, NaN of value 16 db + i
 #pragma unroll 1
         for (pass = 4; pass > 0; --pass) {
-            walk(std::true_type{});
+            walk();
             __syncthreads();  // the tiles are read before they are copied again
 #pragma unroll
             for (int k = 2; k < 5; ++k) {
@@ -763,6 +818,7 @@ __device__ __forceinline__ void attend(const KeySeg& seg, const ScoreArgs& sc, c
             emit(r, dim, v, mm, ll);
         }
     }
+    return true;
 }
 
 __device__ __forceinline__ int clamp_pos(long long x) {

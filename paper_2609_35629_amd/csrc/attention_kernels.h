@@ -6,6 +6,14 @@
 
 namespace santapp {
 
+typedef __attribute__((address_space(3))) char lds_char;
+
+// The kernel's one argument, where it was passed.
+template <typename A>
+__device__ __forceinline__ const A* kernel_args() {
+    return (const A*)__builtin_amdgcn_kernarg_segment_ptr();
+}
+
 // Joins the split parts of rows.  The parts of a row come in up to two runs
 // (prompt, suffix) of at most kMaxParts in all.  Rows of more than kFewParts take a
 // workgroup each, several parts in flight (140 rows of 128 parts: 99 us with a

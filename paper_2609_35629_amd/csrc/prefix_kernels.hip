@@ -27,14 +27,13 @@ struct PrefixShape {
     static constexpr int kPerCu = Prompt::kPerCu < Suffix::kPerCu ? Prompt::kPerCu : Suffix::kPerCu;
 };
 
-template <typename T, int D, int WR, int WK, int MODE>
-__global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) void k_prefix(PrefixArgs a) {
+// The block of rows of this workgroup; attend()'s answer.
+template <typename T, int D, int WR, int WK, int MODE, bool SPECIAL>
+__device__ __forceinline__ bool prefix_block(const PrefixArgs& a, char* buf0, char* buf1) {
     using PS = PrefixShape<T, D, WR, WK>;
     using SH = typename PS::Prompt;
     using SS = typename PS::Suffix;
     constexpr int SK = PS::SK, NT = PS::NT;
-    __shared__ __align__(16) char buf0[PS::kBuf];
-    __shared__ __align__(16) char buf1[PS::kBuf];
     const int Hq = a.Hkv * a.G;
     const int prompts = a.P * a.Hkv * a.row_blocks * a.part.splits;
     int x = blockIdx.x;
@@ -77,10 +76,9 @@ __global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) 
             else
                 store4(a.out + head(r) * D + dim, v, inverse_sum(l));
         };
-        attend<T, D, NT, WR, WK, MODE, true>(seg, a.score, nullptr, nullptr, split, a.part.splits, buf0, buf1,
+        return attend<T, D, NT, WR, WK, MODE, true, SPECIAL>(seg, a.score, nullptr, nullptr, split, a.part.splits, buf0, buf1,
                                               min(SH::BM, R - r0), rowinfo, qrow,
                                             emit);
-        return;
     }
     x -= prompts;
     const int pairs = a.P * a.S * a.Hkv;
@@ -117,8 +115,23 @@ __global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) 
         else
             store4(a.out + head(r) * D + dim, v, inverse_sum(l));
     };
-    attend<T, D, NT, WR * WK / SK, SK, MODE, true>(seg, a.score, nullptr, nullptr, split, a.spart.splits, buf0, buf1,
+    return attend<T, D, NT, WR * WK / SK, SK, MODE, true, SPECIAL>(seg, a.score, nullptr, nullptr, split, a.spart.splits, buf0, buf1,
                                                          min(SS::BM, a.G - r0), rowinfo, qrow, emit);
+}
+
+// Called, not inlined: what it keeps in registers is no burden to the kernel's loop.
+template <typename T, int D, int WR, int WK, int MODE>
+__device__ __attribute__((noinline)) void prefix_special(const PrefixArgs* a, lds_char* buf0, lds_char* buf1) {
+    prefix_block<T, D, WR, WK, MODE, true>(*a, (char*)buf0, (char*)buf1);
+}
+
+template <typename T, int D, int WR, int WK, int MODE>
+__global__ __launch_bounds__(64 * WR * WK, (PrefixShape<T, D, WR, WK>::kPerCu)) void k_prefix(PrefixArgs a) {
+    using PS = PrefixShape<T, D, WR, WK>;
+    __shared__ __align__(16) char buf0[PS::kBuf];
+    __shared__ __align__(16) char buf1[PS::kBuf];
+    if (!prefix_block<T, D, WR, WK, MODE, false>(a, buf0, buf1))
+        prefix_special<T, D, WR, WK, MODE>(kernel_args<PrefixArgs>(), (lds_char*)buf0, (lds_char*)buf1);
 }
 
 template <int D>

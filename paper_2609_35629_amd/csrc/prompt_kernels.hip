@@ -23,11 +23,10 @@ __global__ __launch_bounds__(256) void k_doc_ranges(const int* docs, int B, int 
     if (i % kDocTile == 0) ranges[row * nr + r] = make_int2(lo, hi);
 }
 
-template <typename T, int D, int WR, int WK, int MODE>
-__global__ __launch_bounds__(64 * WR * WK, (Shape<T, D, 1, WR, WK>::kPerCu)) void k_prompt(PromptArgs a) {
+// The block of rows of this workgroup; attend()'s answer.
+template <typename T, int D, int WR, int WK, int MODE, bool SPECIAL>
+__device__ __forceinline__ bool prompt_block(const PromptArgs& a, char* buf0, char* buf1) {
     using SH = Shape<T, D, 1, WR, WK>;
-    __shared__ __align__(16) char buf0[SH::kBuf];
-    __shared__ __align__(16) char buf1[SH::kBuf];
     const int BH = a.B * a.Hkv, R = a.T * a.G;
     // pairs fastest, so that a pair's blocks share an XCD's cache where the
     // pairs divide the XCDs; the last rows (under a causal mask the longest) first
@@ -75,9 +74,24 @@ __global__ __launch_bounds__(64 * WR * WK, (Shape<T, D, 1, WR, WK>::kPerCu)) voi
         store4(reinterpret_cast<T*>(p) + dim, v, inverse_sum(l));
     };
     const int2* ranges = docs ? a.doc_range + static_cast<long long>(b) * ((a.N + kDocTile - 1) / kDocTile) : nullptr;
-    attend<T, D, 1, WR, WK, MODE, sizeof(T) == 4>(seg, a.score, docs, ranges, split, a.part.splits, buf0, buf1,
+    return attend<T, D, 1, WR, WK, MODE, sizeof(T) == 4, SPECIAL>(seg, a.score, docs, ranges, split, a.part.splits, buf0, buf1,
                                                  min(SH::BM, R - r0), rowinfo,
                                                  qrow, emit);
+}
+
+// Called, not inlined: what it keeps in registers is no burden to the kernel's loop.
+template <typename T, int D, int WR, int WK, int MODE>
+__device__ __attribute__((noinline)) void prompt_special(const PromptArgs* a, lds_char* buf0, lds_char* buf1) {
+    prompt_block<T, D, WR, WK, MODE, true>(*a, (char*)buf0, (char*)buf1);
+}
+
+template <typename T, int D, int WR, int WK, int MODE>
+__global__ __launch_bounds__(64 * WR * WK, (Shape<T, D, 1, WR, WK>::kPerCu)) void k_prompt(PromptArgs a) {
+    using SH = Shape<T, D, 1, WR, WK>;
+    __shared__ __align__(16) char buf0[SH::kBuf];
+    __shared__ __align__(16) char buf1[SH::kBuf];
+    if (!prompt_block<T, D, WR, WK, MODE, false>(a, buf0, buf1))
+        prompt_special<T, D, WR, WK, MODE>(kernel_args<PromptArgs>(), (lds_char*)buf0, (lds_char*)buf1);
 }
 
 template <typename T, int D>
