@@ -19,8 +19,8 @@
 //
 // bf16 rows: v_mfma_f32_32x32x16_bf16.  fp32 queries over bf16 rows enter as
 // three bf16 terms each (q and P: 24 bits), so that the result is as exact as
-// fp32 products; bf16 queries as one, with P rounded to bf16 (2^-9, like the
-// output's own rounding).  fp32 rows: v_mfma_f32_32x32x2_f32.
+// fp32 products; bf16 queries as one, with P rounded to bf16 (2^-8 at most, like
+// the output's own rounding).  fp32 rows: v_mfma_f32_32x32x2_f32.
 #pragma once
 
 #include "common.h"
@@ -317,33 +317,35 @@ __device__ __forceinline__ int2 doc_run(const int* docs, const int2* ranges, int
     if (d < 0 || lo >= hi) return make_int2(0, 0);
     const int2 none = make_int2(0, -1);
     const int lane = lane_id(), end = (hi + kDocTile - 1) / kDocTile;
+    constexpr int kAhead = 4;  // loads of 64 ranges under way
     int first = -1, last = -1, some = 0, mixed = 0;
-    for (int r = lo / kDocTile; r < end; r += kWave) {
-        bool on = false, all = false;
-        if (r + lane < end) {
-            const int2 x = ranges[r + lane];
-            on = x.x <= d && x.y >= d;
-            all = x.x == x.y;
+    for (int r = lo / kDocTile; r < end; r += kAhead * kWave) {
+        int2 x[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) x[k] = ranges[min(r + k * kWave + lane, end - 1)];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int rk = r + k * kWave;
+            const bool on = rk + lane < end && x[k].x <= d && x[k].y >= d;
+            const uint64_t s = __ballot(on);
+            if (s == 0) continue;
+            if (first < 0) first = rk + static_cast<int>(__builtin_ctzll(s));
+            last = rk + 63 - static_cast<int>(__builtin_clzll(s));
+            some += static_cast<int>(__builtin_popcountll(s));
+            mixed += static_cast<int>(__builtin_popcountll(__ballot(on && x[k].x != x[k].y)));
         }
-        const uint64_t s = __ballot(on);
-        if (s == 0) continue;
-        if (first < 0) first = r + static_cast<int>(__builtin_ctzll(s));
-        last = r + 63 - static_cast<int>(__builtin_clzll(s));
-        some += static_cast<int>(__builtin_popcountll(s));
-        mixed += static_cast<int>(__builtin_popcountll(__ballot(on && !all)));
     }
     if (first < 0) return make_int2(0, 0);
     if (some != last - first + 1) return none;
+    // bit i: key i of the first range, and of the last, is d's (half a wave each)
+    const int half = lane < kDocTile ? first : last, j = half * kDocTile + (lane & (kDocTile - 1));
+    const uint64_t both = __ballot(j < n && docs[min(j, n - 1)] == d);
     const int2 rf = ranges[first], rl = ranges[last];
     const bool mf = rf.x != rf.y, ml = last != first && rl.x != rl.y;
     if (mixed != (mf ? 1 : 0) + (ml ? 1 : 0)) return none;
-    auto keys = [&](int r) {  // bit i: key i of the range is d's
-        const int j = r * kDocTile + lane;
-        return static_cast<uint32_t>(__ballot(lane < kDocTile && j < n && docs[min(j, n - 1)] == d));
-    };
     int x = first * kDocTile, y = min((last + 1) * kDocTile, n);
     if (mf) {
-        const uint32_t e = keys(first);
+        const uint32_t e = static_cast<uint32_t>(both);
         if (e == 0) return none;
         const int z = __builtin_ctz(e);
         const uint32_t up = e >> z;
@@ -353,7 +355,7 @@ __device__ __forceinline__ int2 doc_run(const int* docs, const int2* ranges, int
         if (last == first) y = x + __builtin_popcount(e);
     }
     if (ml) {
-        const uint32_t e = keys(last);
+        const uint32_t e = static_cast<uint32_t>(both >> 32);
         if (e == 0 || (e & (e + 1)) != 0) return none;
         y = last * kDocTile + __builtin_popcount(e);
     }
@@ -509,7 +511,7 @@ __device__ __forceinline__ bool attend(const KeySeg& seg, const ScoreArgs& sc, c
     // The copies of a tile, in kCopies parts (of one K and one V piece): a wave
     // that issues them in a row waits for the other waves' in the queue, so that
     // they go between the products of the tile before (16384 tokens: 1130 us in a
-    // row, COPYTIME between).
+    // row, 1088 between).
     constexpr int kCopies = SH::kTile / (1024 * NW);
     static_assert((STEP & (STEP - 1)) == 0 && kCopies * STEP == BK, "whole groups");
     const char *kb = nullptr, *vb = nullptr;
