@@ -488,7 +488,10 @@ santapp_status santapp_prompt_attention(const santapp_score* score, const santap
                                         const int* prefix, const santapp_rows* out, void* workspace,
                                         size_t ws_bytes, void* stream);
 
-/* Workspace of santapp_prefix_decode with these sizes (bytes, host-only query). */
+/*
+ * Workspace of santapp_prefix_decode with these sizes and any smaller T (bytes,
+ * host-only query).
+ */
 santapp_status santapp_prefix_workspace_bytes(int P, int S, int Hq, int Hkv, int N, int T, int d,
                                               santapp_dtype dtype, size_t* bytes);
 

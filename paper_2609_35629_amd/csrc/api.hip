@@ -1498,7 +1498,8 @@ santapp_status santapp_prefix_decode(const santapp_score* score, const float* q,
     a.prefix_lengths = prefix_lengths;
     a.lengths = lengths;
     a.positions = positions;
-    const size_t need = plan_prefix(a, device_cus(), static_cast<char*>(workspace));
+    static char none[16];  // stands for a workspace that is not needed
+    const size_t need = plan_prefix(a, device_cus(), workspace ? static_cast<char*>(workspace) : none);
     if (need > 0 && (!workspace || ws_bytes < need))
         return fail(SANTAPP_EWORKSPACE, "workspace of %zu bytes needed (got %zu)", need, workspace ? ws_bytes : 0);
     const hipError_t e = launch_prefix(a, static_cast<hipStream_t>(stream));

@@ -378,7 +378,8 @@ constexpr int kDocTile = 32;  // keys per document range
 constexpr long long kMaxRowStep = 1ll << 26;  // bytes between the key rows of a pair
 
 // Launch shapes (host arithmetic only): the variant, row blocks and splits of
-// `a`, and the workspace bytes they need; with `ws`, the places in it.
+// `a`, their places in the workspace at `ws` and its bytes; with ws null, the
+// bytes to have (plan_prefix: for this and any shorter suffix).
 size_t plan_prompt(PromptArgs& a, int cus, char* ws);
 size_t plan_prefix(PrefixArgs& a, int cus, char* ws);
 

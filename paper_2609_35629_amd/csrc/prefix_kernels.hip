@@ -180,6 +180,13 @@ hipError_t launch(const PrefixArgs& a, hipStream_t s) {
 
 }  // namespace
 
+namespace {
+// The most splits of the prompts that are considered: two rounds of blocks.
+long long most_splits(long long tiles, long long slots, long long blocks) {
+    return std::min<long long>(std::min<long long>(tiles, 256), std::max<long long>(1, 2 * slots / blocks));
+}
+}  // namespace
+
 size_t plan_prefix(PrefixArgs& a, int cus, char* ws) {
     if (cus <= 0) cus = 256;
     const bool f32 = a.dtype == SANTAPP_FP32;
@@ -213,7 +220,7 @@ size_t plan_prefix(PrefixArgs& a, int cus, char* ws) {
         const long long tiles = (a.N + bk - 1) / bk, ns = sblocks * a.spart.splits;
         const long long scost = 2 + (ns ? ((a.T + 32 * kw - 1) / (32 * kw) + a.spart.splits - 1) / a.spart.splits : 0);
         long long best = -1;
-        const long long most = std::min<long long>(std::min<long long>(tiles, 256), std::max<long long>(1, 4 * slots / blocks));
+        const long long most = most_splits(tiles, slots, blocks);
         for (long long k = 1; k <= most; ++k) {
             const long long cost = 2 + (tiles + k - 1) / k, rounds = (blocks * k + slots - 1) / slots;
             const long long idle = rounds * slots - blocks * k, more = ns > idle ? (ns - idle + slots - 1) / slots : 0;
@@ -223,6 +230,14 @@ size_t plan_prefix(PrefixArgs& a, int cus, char* ws) {
                 a.part.splits = static_cast<int>(k);
             }
         }
+    }
+    if (!ws) {  // room for any shorter suffix too, whatever splits it leads to
+        PartArgs p = a.part;
+        if (blocks > 0) p.splits = static_cast<int>(most_splits((a.N + bk - 1) / bk, slots, blocks));
+        size_t at = 0;
+        if (p.splits) at += place_parts(p, pairs, R, a.d, ws, at);
+        if (a.spart.splits) at += place_parts(a.spart, pairs * a.S, a.G, a.d, ws, at);
+        return at;
     }
     if (a.part.splits + a.spart.splits <= 1) return 0;
     size_t at = 0;
