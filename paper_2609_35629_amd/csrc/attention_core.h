@@ -20,7 +20,7 @@
 // bf16 rows: v_mfma_f32_32x32x16_bf16.  fp32 queries over bf16 rows enter as
 // three bf16 terms each (q and P: 24 bits), so that the result is as exact as
 // fp32 products; bf16 queries as one, with P rounded to bf16 (2^-8 at most, like
-// the output's own rounding).  fp32 rows: v_mfma_f32_32x32x2_f32.
+// the output's own rounding) or, where rows are few, two terms of it.  fp32 rows: v_mfma_f32_32x32x2_f32.
 #pragma once
 
 #include "common.h"
@@ -112,12 +112,13 @@ struct Tile {
     }
 };
 
-// Query rows as right operands, scores and value sums of 32 keys.
-template <typename T, int D, int NT>
+// Query rows as right operands, scores and value sums of 32 keys.  NT, PT: bf16
+// terms of a query and of a weight.
+template <typename T, int D, int NT, int PT>
 struct Ops;
 
-template <int D, int NT>
-struct Ops<bf16_t, D, NT> {
+template <int D, int NT, int PT>
+struct Ops<bf16_t, D, NT, PT> {
     using TL = Tile<bf16_t, D>;
     bf16x8 q[NT][D / 16];
 
@@ -212,19 +213,19 @@ struct Ops<bf16_t, D, NT> {
                 for (int db = 0; db < D / 32; ++db) a[(k + 1) & 1][db] = values(vtile, row0 + 16 * (k + 1), db, lane);
             }
             __builtin_amdgcn_sched_barrier(0);
-            bf16x8 b[NT];
+            bf16x8 b[PT];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float x = p[k / 2][8 * (k & 1) + e];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
+                for (int t = 0; t < PT; ++t) {
                     const __bf16 h = static_cast<__bf16>(x);
                     b[t][e] = h;
                     x -= static_cast<float>(h);
                 }
             }
 #pragma unroll
-            for (int t = NT - 1; t >= 0; --t)
+            for (int t = PT - 1; t >= 0; --t)
 #pragma unroll
                 for (int db = 0; db < D / 32; ++db)
                     o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[k & 1][db], b[t], o[db], 0, 0, 0);
@@ -233,7 +234,7 @@ struct Ops<bf16_t, D, NT> {
 };
 
 template <int D>
-struct Ops<float, D, 1> {
+struct Ops<float, D, 1, 1> {
     using TL = Tile<float, D>;
     // dims 8 c + 4 (lane / 32) + e of the row, as q[c].e
     float4 q[D / 8];
@@ -407,7 +408,10 @@ __device__ __forceinline__ bool attend(const KeySeg& seg, const ScoreArgs& sc, c
                                        Emit&& emit) {
     using SH = Shape<T, D, NT, WR, WK>;
     using TL = Tile<T, D>;
-    using OP = Ops<T, D, NT>;
+    // bf16 queries: one term of a weight, where rows are few (blocks of 32 by four
+    // waves over keys, which wait for memory) two
+    constexpr int PT = sizeof(T) == 2 && NT == 1 && WK == 4 ? 2 : NT;
+    using OP = Ops<T, D, NT, PT>;
     constexpr int BK = SH::BK, KS = SH::KS, NW = SH::NW, SUB = SH::SUB;
     constexpr bool EXTRA = (MODE & kExtra) != 0, DOCS = (MODE & kDocs) != 0;
     const int lane = lane_id(), hh = lane >> 5;
