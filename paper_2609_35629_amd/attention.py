@@ -92,18 +92,23 @@ def _heads(t: torch.Tensor, name: str) -> torch.Tensor:
     return t.unsqueeze(2)
 
 
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """A new tensor of the stream that will write it: memory of another
+    stream's could still be in use there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _scratch(workspace: Optional[torch.Tensor], size, device, stream):
     """Address and bytes of the caller's workspace, or of a new one of
-    ``size()`` bytes.  On a stream of the caller's, which need not be the
-    current one, a new one must not be given out again before that stream has
-    passed the call."""
+    ``size()`` bytes (and that tensor)."""
     if workspace is None:
         need = size()
         if not need:
             return None, 0, None
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        if stream is not None:
-            workspace.record_stream(stream)
+        workspace = _empty(need, torch.uint8, device, stream)
         return workspace.data_ptr(), need, workspace
     if workspace.device != device or not workspace.is_contiguous():
         _misfit(workspace, "workspace", workspace.shape, device, workspace.dtype)
@@ -166,9 +171,7 @@ def rope(x: torch.Tensor, freqs: torch.Tensor, positions: Optional[torch.Tensor]
     device, current, s = _on(x, "x", stream)
     x4 = _heads(x, "x")
     if out is None:
-        out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=device)
-        if stream is not None:
-            out.record_stream(stream)
+        out = _empty(x.shape, out_dtype or x.dtype, device, stream)
     elif out_dtype is not None and out.dtype != out_dtype:
         _fail(f"out has dtype {out.dtype}, expected {out_dtype}")
     o4 = _heads(out, "out")
@@ -179,7 +182,7 @@ def rope(x: torch.Tensor, freqs: torch.Tensor, positions: Optional[torch.Tensor]
     pos = _array(positions, "positions", (B, T), torch.int32, device)
     r = _rotation(freqs, interleaved, magnitude, device)
     _call(device, current, _lib.load().santapp_rope, r, _rows(x4, "x", shape, device), _code(x, "x"), B, H, T, d, pos,
-          first, _rows(o4, "out", shape, device), _code(out, "out"), s)
+          int(first), _rows(o4, "out", shape, device), _code(out, "out"), s)
     return out
 
 
@@ -210,9 +213,7 @@ def rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cac
         q4 = _heads(q, "q")
         Hq = q4.shape[1]
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=torch.float32, device=device)
-            if stream is not None:
-                q_out.record_stream(stream)
+            q_out = _empty(q.shape, torch.float32, device, stream)
         qs = (B, Hq, T, d)
         qr, qo = _rows(q4, "q", qs, device), _rows(_heads(q_out, "q_out"), "q_out", qs, device)
         qc, oc = _code(q, "q"), _code(q_out, "q_out")
@@ -222,14 +223,14 @@ def rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cac
     if isinstance(at, torch.Tensor):
         rows = _array(at, "at", (B,), torch.int32, device)
     else:
-        row0 = at
+        row0 = int(at)
     if positions is not None and positions.dim() == 1:
         positions = positions.unsqueeze(1)
     pos = _array(positions, "positions", (B, T), torch.int32, device)
     _call(device, current, _lib.load().santapp_rope_append, _rotation(freqs, interleaved, magnitude, device), qr, qc, qo,
           oc, _rows(k4, "k", shape, device), _rows(v4, "v", shape, device), _code(k, "k"),
           _rows(cache_K, "cache_K", held, device), _rows(cache_V, "cache_V", held, device), _code(cache_K, "cache_K"), cap,
-          B, Hq, Hkv, T, d, rows, row0, pos, first, s)
+          B, Hq, Hkv, T, d, rows, row0, pos, int(first), s)
     return q_out
 
 
@@ -239,7 +240,7 @@ def rope_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cac
 
 
 def _score(scale, softcap, slopes, window, Hq, device) -> _lib.Score:
-    return _lib.Score(scale, softcap, _array(slopes, "slopes", (Hq,), torch.float32, device), window)
+    return _lib.Score(scale, softcap, _array(slopes, "slopes", (Hq,), torch.float32, device), int(window))
 
 
 def prompt_workspace(B: int, Hq: int, Hkv: int, T: int, N: int, d: int, dtype: torch.dtype = torch.bfloat16,
@@ -285,9 +286,11 @@ def prompt_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, causal: 
     if offset is None:
         offset = N - T if N >= T or causal else 0
     if out is None:
-        out = torch.empty_like(q)  # q's order of dimensions where q is dense
-        if stream is not None:
-            out.record_stream(stream)
+        if stream is None:
+            out = torch.empty_like(q)  # q's order of dimensions where q is dense
+        else:
+            with torch.cuda.stream(stream):
+                out = torch.empty_like(q)
     elif out.dtype != dtype:
         _fail(f"out has dtype {out.dtype}, expected {dtype}")
     keys = (B, Hkv, N, d)
@@ -299,11 +302,11 @@ def prompt_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, causal: 
 
     def size():
         n = ctypes.c_size_t()
-        _call(device, current, lib.santapp_prompt_workspace_bytes, B, Hq, Hkv, T, N, d, code, window, docs is not None, n)
+        _call(device, current, lib.santapp_prompt_workspace_bytes, B, Hq, Hkv, T, N, d, code, int(window), docs is not None, n)
         return n.value
     ws, ws_bytes, hold = _scratch(workspace, size, device, stream)
     _call(device, current, lib.santapp_prompt_attention, _score(scale, softcap, slopes, window, Hq, device), qr, kr, vr, code,
-          B, Hq, Hkv, T, N, d, bool(causal), offset, docs, pre, orr, ws, ws_bytes, s)
+          B, Hq, Hkv, T, N, d, bool(causal), int(offset), docs, pre, orr, ws, ws_bytes, s)
     return out
 
 
@@ -356,14 +359,11 @@ def prefix_decode(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, suffix_K: O
         cap = suffix_K.shape[2]
         held = (B, Hkv, cap, d)
         sk, sv = _rows(suffix_K, "suffix_K", held, device), _rows(suffix_V, "suffix_V", held, device)
-        if T is None:
-            T = cap
-        elif T < 0 or T > cap:
+        T = cap if T is None else int(T)
+        if T < 0 or T > cap:
             _fail(f"T={T} outside the suffix buffer's {cap} rows")
     if out is None:
-        out = torch.empty(shape, dtype=torch.float32, device=device)
-        if stream is not None:
-            out.record_stream(stream)
+        out = _empty(shape, torch.float32, device, stream)
     keys = (P, Hkv, N, d)
     kr, vr = _rows(K, "K", keys, device), _rows(V, "V", keys, device)
     lib = _lib.load()

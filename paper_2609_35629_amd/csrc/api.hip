@@ -1374,7 +1374,8 @@ static santapp_status prompt_sizes(int B, int Hq, int Hkv, int T, int N, int d, 
     if (!dtype_ok(dtype)) return fail(SANTAPP_EDTYPE, "unsupported dtype %d", static_cast<int>(dtype));
     if (santapp_status st = check_head_dim(d)) return st;
     if (N >= kMaxKeys) return fail(SANTAPP_ELIMIT, "N must be below 2^24");
-    if (static_cast<long long>(T) * (Hq / Hkv) >= kMaxRows || static_cast<long long>(T) * Hq * B / 32 >= kMaxRows)
+    if (static_cast<long long>(T) * (Hq / Hkv) >= kMaxRows || static_cast<long long>(B) * Hq >= kMaxRows ||
+        static_cast<long long>(B) * Hq / 32 * T >= kMaxRows)
         return fail(SANTAPP_ELIMIT, "too many rows");
     a->B = B;
     a->Hkv = Hkv;

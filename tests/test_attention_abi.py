@@ -118,6 +118,7 @@ def test_prompt_refusals():
     refused(call(d=80), "head dim", _lib.ELIMIT)
     refused(call(N=1 << 24, offset=0), "2^24", _lib.ELIMIT)
     refused(call(T=1 << 29, N=1 << 23, causal=0), "too many rows", _lib.ELIMIT)
+    refused(call(B=1 << 20, Hq=1 << 12, Hkv=1 << 12, T=1, offset=0), "too many rows", _lib.ELIMIT)
     for bad in (dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan")), dict(scale=1e-39), dict(scale=1e31)):
         refused(call(sc=score(**bad)), "scale")
     for bad in (-1.0, float("nan"), 1e-35, 1e32):
