@@ -13,6 +13,7 @@
 #include <string>
 #include <vector>
 
+#include "attention.h"
 #include "internal.h"
 
 struct santapp_teams {

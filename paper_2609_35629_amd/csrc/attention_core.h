@@ -23,8 +23,8 @@
 // the output's own rounding) or, where rows are few, two terms of it.  fp32 rows: v_mfma_f32_32x32x2_f32.
 #pragma once
 
+#include "attention.h"
 #include "common.h"
-#include "internal.h"
 
 #include <type_traits>
 

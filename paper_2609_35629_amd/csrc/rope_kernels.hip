@@ -14,8 +14,8 @@
 // looked at for every row it took 150 us.
 #include <type_traits>
 
+#include "attention.h"
 #include "common.h"
-#include "internal.h"
 
 namespace santapp {
 
