@@ -20,7 +20,16 @@
 // bf16 rows: v_mfma_f32_32x32x16_bf16.  fp32 queries over bf16 rows enter as
 // three bf16 terms each (q and P: 24 bits), so that the result is as exact as
 // fp32 products; bf16 queries as one, with P rounded to bf16 (2^-8 at most, like
-// the output's own rounding) or, where rows are few, two terms of it.  fp32 rows: v_mfma_f32_32x32x2_f32.
+// the output's own rounding) or, where rows are few, two terms of it.  fp32 rows:
+// v_mfma_f32_32x32x2_f32.
+//
+// Bound: the matrix cores where rows are many, memory where they are few.  A wave's
+// step of 64 keys of 128 dims is 1024 cycles of products and about 950 of softmax,
+// which run beside each other only between the two waves of a SIMD: 16384 causal
+// tokens of 16 heads take 1055 us (1040 TFLOP/s; a bf16 matrix product of 8192^3
+// reaches 1170 on the same card).  Few rows: 67 MB of a 32K prompt's cache for eight
+// answers in 28 us, of which the start and end of a block and the join of its
+// parts are about 13.
 #pragma once
 
 #include "attention.h"
@@ -553,8 +562,11 @@ __device__ __forceinline__ bool attend(const KeySeg& seg, const ScoreArgs& sc, c
     // emitted) is done again with SPECIAL, which walks the tiles four times: in
     // passes 4, 3, 2 over V's NaNs, -infinities and +infinities as ones, with ones
     // for the weights of unmasked keys, which says where they belong (has[]), and in
-    // pass 1 over V with zeros in their place.
+    // pass 1 over V with zeros in their place.  Sums that still are not finite
+    // (values near the largest number, times weights above 1) are walked once more
+    // with the reference at the maximum throughout.
     int pass = 0;
+    float slack = 8.f;
     auto compute = [&](int t, int sub, const char* buf, bool alone, auto&& between) {
         const int in_tile = sub * SH::kStep + wk * 32 * KS;  // the wave's first key of the step
         const int k0 = t * BK + in_tile;
@@ -634,7 +646,7 @@ __device__ __forceinline__ bool attend(const KeySeg& seg, const ScoreArgs& sc, c
         if constexpr (!EXTRA) top *= sc.scale_log2;
         // the reference m moves only where a score exceeds it by more than 8
         // (weights up to 2^8 are as exact as those below 1)
-        if (__any(top > m + 8.f)) {
+        if (__any(top > m + (SPECIAL ? slack : 8.f))) {
             const float mn = fmaxf(m, top);
             const float f = mn == kNegInf || (SPECIAL && pass > 1) ? 1.f : exp2_fast(m - mn);
             l *= f;
@@ -729,16 +741,20 @@ __device__ __forceinline__ bool attend(const KeySeg& seg, const ScoreArgs& sc, c
             alone = (same >> (t - seen)) & 1;
         }
     };
-    if constexpr (!SPECIAL) {
-        __shared__ int s_special;
-        if (threadIdx.x == 0) s_special = 0;  // before the first tile's barrier; without tiles no value is special
-        walk();
+    // whether some sum of the wave's rows is not finite
+    auto overflows = [&]() {
         float z = 0.f;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
             for (int i = 0; i < 16; ++i) z = fmaf(o[db][i], 0.f, z);
-        if (__any(mine && z != 0.f) && lane == 0) s_special = 1;
+        return __any(mine && z != 0.f) != 0;
+    };
+    if constexpr (!SPECIAL) {
+        __shared__ int s_special;
+        if (threadIdx.x == 0) s_special = 0;  // before the first tile's barrier; without tiles no value is special
+        walk();
+        if (overflows() && lane == 0) s_special = 1;
         __syncthreads();
         if (s_special) return false;  // uniform
     } else {
@@ -758,6 +774,12 @@ __device__ __forceinline__ bool attend(const KeySeg& seg, const ScoreArgs& sc, c
                     has[k - 2][w] = bits;
                 }
             }
+        }
+        if (__syncthreads_or(overflows())) {
+            pass = 1;
+            slack = 0.f;
+            walk();
+            __syncthreads();
         }
 #pragma unroll
         for (int w = 0; w < D / 64; ++w)
@@ -790,16 +812,16 @@ __device__ __forceinline__ bool attend(const KeySeg& seg, const ScoreArgs& sc, c
             constexpr int HALF = (NW + 1) / 2;
             return reinterpret_cast<float*>((w < HALF ? buf0 : buf1) + (w < HALF ? w : w - HALF) * SH::kState);
         };
-        float* mine = state(wv) + (lane & 31) * ST;
+        float* own = state(wv) + (lane & 31) * ST;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<float4*>(mine + 32 * db + 2 * i + 4 * hh) =
+                *reinterpret_cast<float4*>(own + 32 * db + 2 * i + 4 * hh) =
                     make_float4(o[db][i], o[db][i + 1], o[db][i + 2], o[db][i + 3]);
         if (hh == 0) {
-            mine[D] = m;
-            mine[D + 1] = l;
+            own[D] = m;
+            own[D + 1] = l;
         }
         __syncthreads();
         for (int x = threadIdx.x; x < SH::BM * (D / 4); x += NW * kWave) {

@@ -185,6 +185,22 @@ def test_large_scores(dtype):
     assert torch.isfinite(out).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("T", [1, 200])
+def test_values_near_the_largest_number(dtype, T):
+    # key 100 scores 5 above the others and holds 2^127: its weight, below one,
+    # must not overflow on the way to a finite result
+    N, d = 200, 64
+    q, K, V = torch.zeros(1, 1, T, d, dtype=dtype), torch.zeros(1, 1, N, d, dtype=dtype), _rand((1, 1, N, d), dtype, 1)
+    q[..., 0] = 8.0
+    K[0, 0, 100, 0] = 5.0
+    V[0, 0, 100] = 2.0 ** 127
+    out = sp.prompt_attention(q.cuda(), K.cuda(), V.cuda(), causal=False).cpu().double()
+    w = math.exp(5.0) / (math.exp(5.0) + N - 1)
+    # the weights' rounding and the result's, and a few of fp32
+    assert ((out - w * 2.0 ** 127).abs() <= w * 2.0 ** 127 * (2 * ref.HALF[dtype] + 64 * ref.F32)).all()
+
+
 def test_views_and_repeated_rows():
     B, Hq, Hkv, T, d = 2, 6, 2, 150, 128
     qkv = _rand((B, T, Hq + 2 * Hkv, d), BF, 1).cuda()  # as one projection leaves them
