@@ -11,7 +11,8 @@
 // that the angles (about 60 instructions a pair) stay beside the row traffic:
 // 470 MB of a 32K prompt's queries in 87 us (5.4 TB/s; a plain copy moves 4.9).
 // A kernel of its own for one stream with its types known: with the types
-// looked at for every row it took 150 us.
+// looked at for every row it took 150 us.  The streams of an append, a few rows
+// each, take that one (4 us, a launch's start and end).
 #include <type_traits>
 
 #include "attention.h"
@@ -40,18 +41,7 @@ __device__ __forceinline__ void turn(double p, double f, float& sn, float& cs) {
     cs = (n == 1 || n == 2) ? -b : b;
 }
 
-__device__ __forceinline__ float load1(const void* p, bool f32, long long i) {
-    return f32 ? static_cast<const float*>(p)[i] : bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
-}
-
 __device__ __forceinline__ uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); }
-
-__device__ __forceinline__ void store1(void* p, bool f32, long long i, float v) {
-    if (f32)
-        static_cast<float*>(p)[i] = v;
-    else
-        static_cast<uint16_t*>(p)[i] = to_bf16(v);
-}
 
 // Eight consecutive elements, 16-byte aligned.
 __device__ __forceinline__ void load8(const void* p, bool f32, long long i, float (&v)[8]) {
@@ -120,99 +110,71 @@ struct Eight<true> {
     }
 };
 
-// x, y: the halves of eight pairs (or, interleaved, the pairs one after the other).
-__device__ __forceinline__ void turn8(float (&x)[8], float (&y)[8], const float (&sn)[8], const float (&cs)[8],
-                                      bool interleaved) {
-    if (interleaved) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float u = x[2 * e], w = x[2 * e + 1];
-            x[2 * e] = u * cs[e] - w * sn[e];
-            x[2 * e + 1] = w * cs[e] + u * sn[e];
-            const float u2 = y[2 * e], w2 = y[2 * e + 1];
-            y[2 * e] = u2 * cs[e + 4] - w2 * sn[e + 4];
-            y[2 * e + 1] = w2 * cs[e + 4] + u2 * sn[e + 4];
-        }
-    } else {
+// The eight elements 8 unit .. of a row, and how each is turned: by cs and sn and
+// its partner's place in the row (-1: an element that is copied).
+struct Turns {
+    float sn[8], cs[8];
+    int other[8];
+    __device__ __forceinline__ void set(const RopeArgs& a, int unit, long long pos) {
+        const int R = a.pairs;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float u = x[e], w = y[e];
-            x[e] = u * cs[e] - w * sn[e];
-            y[e] = w * cs[e] + u * sn[e];
+            const int j = 8 * unit + e;
+            const bool second = a.interleaved ? (j & 1) != 0 : j >= R;
+            other[e] = j >= 2 * R ? -1 : a.interleaved ? j ^ 1 : second ? j - R : j + R;
+            const int f = j >= 2 * R ? 0 : a.interleaved ? j >> 1 : second ? j - R : j;
+            turn(static_cast<double>(pos), a.freqs[f], sn[e], cs[e]);
+            cs[e] *= a.magnitude;
+            sn[e] *= second ? a.magnitude : -a.magnitude;
         }
     }
-}
+    // The partners meet in LDS: `mine` is this thread's 32 bytes of its row's.
+    __device__ __forceinline__ void apply(float (&u)[8], float4* mine, const float* row, bool rotate) const {
+        mine[0] = make_float4(u[0], u[1], u[2], u[3]);
+        mine[1] = make_float4(u[4], u[5], u[6], u[7]);
+        wave_lds_sync();
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (rotate && other[e] >= 0) u[e] = u[e] * cs[e] + row[other[e]] * sn[e];
+        wave_lds_sync();
+    }
+};
 
-// One thread: one token (b, t), one unit of the row and the heads
-// h0, h0 + hstep, .. of all streams.  VEC: a unit is eight pairs, or eight
-// dims that are not rotated (16-byte accesses); otherwise one pair or one dim.
-template <bool VEC>
+// Several streams, of any types and pairs: one thread, one token (b, t), eight
+// elements of a row (the d / 8 lanes of a row are lanes of one wave) and the
+// heads h0, h0 + hstep, .. of all streams.
 __global__ __launch_bounds__(kThreads) void k_rope(RopeArgs a) {
-    constexpr int E = VEC ? kPairs : 1;
-    const int R = a.pairs, rot_units = VEC ? R / kPairs : R;
-    const int units = rot_units + (a.d - 2 * R) / E;
+    __shared__ float4 s_row[2 * kThreads];
+    const int units = a.d / 8;
+    const unsigned per_token = static_cast<unsigned>(units) * a.hstep;
     const long long i = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
-    const long long per_token = static_cast<long long>(units) * a.hstep;
     const long long token = i / per_token;
-    if (token >= static_cast<long long>(a.B) * a.T) return;
-    const int rest = static_cast<int>(i - token * per_token);
-    const int h0 = rest / units, unit = rest - h0 * units;
+    if (token >= static_cast<long long>(a.B) * a.T) return;  // whole rows
+    const unsigned rest = static_cast<unsigned>(i - token * per_token);
+    const int h0 = rest / static_cast<unsigned>(units), unit = rest - h0 * units;
     const int b = static_cast<int>(token / a.T), t = static_cast<int>(token - static_cast<long long>(b) * a.T);
     const long long row = (a.at ? a.at[b] : a.at0) + static_cast<long long>(t);
     const bool fits = row >= 0 && row < a.capacity;  // of the streams that are appended
-    const bool rotated = unit < rot_units;
-    // the unit's first dims: the pair's halves, or the dims copied
-    int d1, d2;
-    if (rotated) {
-        d1 = a.interleaved ? 2 * E * unit : E * unit;
-        d2 = a.interleaved ? d1 + E : d1 + R;
-    } else {
-        d1 = d2 = 2 * R + E * (unit - rot_units);
-    }
-    float sn[E], cs[E];
-    if (rotated) {
-        const long long pos = a.positions ? static_cast<long long>(a.positions[token]) : a.first + row;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            turn(static_cast<double>(pos), a.freqs[E * unit + e], sn[e], cs[e]);
-            sn[e] *= a.magnitude;
-            cs[e] *= a.magnitude;
-        }
-    }
+    Turns turns;
+    turns.set(a, unit, a.positions ? static_cast<long long>(a.positions[token]) : a.first + row);
     for (int h = h0; h < a.heads; h += a.hstep) {
         const int si = h < a.s[0].heads ? 0 : h < a.s[0].heads + a.s[1].heads ? 1 : 2;
         const RopeStream& s = a.s[si];
         const int hs = h - (si > 0 ? a.s[0].heads : 0) - (si > 1 ? a.s[1].heads : 0);
         if (s.append && !fits) continue;
-        const long long in = b * s.ib + hs * s.ih + t * s.it;
-        const long long out = b * s.ob + hs * s.oh + (s.append ? row : t) * s.ot;
-        if constexpr (VEC) {
-            float x[8], y[8];
-            load8(s.in, s.in32, in + d1, x);
-            if (rotated) load8(s.in, s.in32, in + d2, y);
-            if (rotated && s.rotate) turn8(x, y, sn, cs, a.interleaved);
-            store8(s.out, s.out32, out + d1, x);
-            if (rotated) store8(s.out, s.out32, out + d2, y);
-        } else {
-            float x = load1(s.in, s.in32, in + d1), y = 0.f;
-            if (rotated) y = load1(s.in, s.in32, in + d2);
-            if (rotated && s.rotate) {
-                const float u = x, w = y;
-                x = u * cs[0] - w * sn[0];
-                y = w * cs[0] + u * sn[0];
-            }
-            store1(s.out, s.out32, out + d1, x);
-            if (rotated) store1(s.out, s.out32, out + d2, y);
-        }
+        float u[8];
+        load8(s.in, s.in32, b * s.ib + hs * s.ih + t * s.it + 8 * unit, u);
+        turns.apply(u, s_row + 2 * threadIdx.x, reinterpret_cast<const float*>(s_row + 2 * (threadIdx.x - unit)), s.rotate);
+        store8(s.out, s.out32, b * s.ob + hs * s.oh + (s.append ? row : t) * s.ot + 8 * unit, u);
     }
 }
 
-// One stream of rows whose pairs come in whole units (d / 8 - pairs / 8 units a
-// row): one thread, one token and unit, heads h0, h0 + hstep, .., the next
+// One stream of rows rotated whole, in halves (2 pairs == d, d / 16 units of eight
+// pairs a row): one thread, one token and unit, heads h0, h0 + hstep, .., the next
 // head's elements in flight while one is turned and stored.
-template <bool IN32, bool OUT32, bool INTER>
+template <bool IN32, bool OUT32>
 __global__ __launch_bounds__(kThreads) void k_rope_rows(RopeArgs a) {
-    const int R = a.pairs, rot_units = R / kPairs, units = a.d / 8 - rot_units;
+    const int R = a.pairs, units = R / kPairs;
     const unsigned per_token = static_cast<unsigned>(units) * a.hstep;
     const long long i = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
     const long long token = i / per_token;
@@ -220,43 +182,73 @@ __global__ __launch_bounds__(kThreads) void k_rope_rows(RopeArgs a) {
     const unsigned rest = static_cast<unsigned>(i - token * per_token);
     const int h0 = rest / static_cast<unsigned>(units), unit = rest - h0 * units;
     const int b = static_cast<int>(token / a.T), t = static_cast<int>(token - static_cast<long long>(b) * a.T);
-    const bool rotated = unit < rot_units;
-    const int d1 = !rotated ? 2 * R + 8 * (unit - rot_units) : INTER ? 16 * unit : 8 * unit;
-    const int d2 = INTER ? d1 + 8 : d1 + R;
     const RopeStream& s = a.s[0];
-    long long in = b * s.ib + h0 * s.ih + t * s.it, out = b * s.ob + h0 * s.oh + t * s.ot;
+    long long in = b * s.ib + h0 * s.ih + t * s.it + 8 * unit, out = b * s.ob + h0 * s.oh + t * s.ot + 8 * unit;
     Eight<IN32> x, y;
-    x.load(s.in, in + d1);
-    y = x;
-    if (rotated) y.load(s.in, in + d2);
+    x.load(s.in, in);
+    y.load(s.in, in + R);
+    const long long pos = a.positions ? static_cast<long long>(a.positions[token]) : a.first + t;
     float sn[8], cs[8];
-    if (rotated) {
-        const long long pos = a.positions ? static_cast<long long>(a.positions[token]) : a.first + t;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            turn(static_cast<double>(pos), a.freqs[8 * unit + e], sn[e], cs[e]);
-            sn[e] *= a.magnitude;
-            cs[e] *= a.magnitude;
-        }
+    for (int e = 0; e < 8; ++e) {
+        turn(static_cast<double>(pos), a.freqs[8 * unit + e], sn[e], cs[e]);
+        sn[e] *= a.magnitude;
+        cs[e] *= a.magnitude;
     }
     for (int h = h0; h < a.heads; h += a.hstep) {
         Eight<IN32> nx = x, ny = y;
         in += a.hstep * s.ih;
         if (h + a.hstep < a.heads) {
-            nx.load(s.in, in + d1);
-            if (rotated) ny.load(s.in, in + d2);
+            nx.load(s.in, in);
+            ny.load(s.in, in + R);
         }
         float u[8], w[8];
         x.get(u);
-        if (rotated) {
-            y.get(w);
-            turn8(u, w, sn, cs, INTER);
-            Eight<OUT32>::store(s.out, out + d2, w);
+        y.get(w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float p = u[e], q = w[e];
+            u[e] = p * cs[e] - q * sn[e];
+            w[e] = q * cs[e] + p * sn[e];
         }
-        Eight<OUT32>::store(s.out, out + d1, u);
+        Eight<OUT32>::store(s.out, out, u);
+        Eight<OUT32>::store(s.out, out + R, w);
         out += a.hstep * s.oh;
         x = nx;
         y = ny;
+    }
+}
+
+// One stream of rows with other pairs, as k_rope: 8192 tokens of 28 heads of 128,
+// bf16, in 23 us whatever the pairs (rows rotated whole in halves, as above: 22;
+// with interleaved pairs in one thread, read at 32-byte steps: 39).
+template <bool IN32, bool OUT32>
+__global__ __launch_bounds__(kThreads) void k_rope_any(RopeArgs a) {
+    __shared__ float4 s_row[2 * kThreads];
+    const int units = a.d / 8;
+    const unsigned per_token = static_cast<unsigned>(units) * a.hstep;
+    const long long i = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
+    const long long token = i / per_token;
+    if (token >= static_cast<long long>(a.B) * a.T) return;  // whole rows
+    const unsigned rest = static_cast<unsigned>(i - token * per_token);
+    const int h0 = rest / static_cast<unsigned>(units), unit = rest - h0 * units;
+    const int b = static_cast<int>(token / a.T), t = static_cast<int>(token - static_cast<long long>(b) * a.T);
+    const RopeStream& s = a.s[0];
+    long long in = b * s.ib + h0 * s.ih + t * s.it + 8 * unit, out = b * s.ob + h0 * s.oh + t * s.ot + 8 * unit;
+    Eight<IN32> x;
+    x.load(s.in, in);
+    Turns turns;
+    turns.set(a, unit, a.positions ? static_cast<long long>(a.positions[token]) : a.first + t);
+    for (int h = h0; h < a.heads; h += a.hstep) {
+        Eight<IN32> nx = x;
+        in += a.hstep * s.ih;
+        if (h + a.hstep < a.heads) nx.load(s.in, in);
+        float u[8];
+        x.get(u);
+        turns.apply(u, s_row + 2 * threadIdx.x, reinterpret_cast<const float*>(s_row + 2 * (threadIdx.x - unit)), true);
+        Eight<OUT32>::store(s.out, out, u);
+        out += a.hstep * s.oh;
+        x = nx;
     }
 }
 
@@ -266,10 +258,8 @@ hipError_t launch_rope(RopeArgs a, int cus, hipStream_t s) {
     a.heads = a.s[0].heads + a.s[1].heads + a.s[2].heads;
     const long long tokens = static_cast<long long>(a.B) * a.T;
     if (tokens == 0 || a.heads == 0) return hipSuccess;
-    // 16-byte units need the second half of the pairs, and what is copied
-    // behind them, to start on one
-    const bool vec = a.pairs % kPairs == 0;
-    const int units = vec ? a.d / 8 - a.pairs / kPairs : a.d - a.pairs;
+    const bool one = a.s[1].heads == 0, halves = one && !a.interleaved && 2 * a.pairs == a.d;
+    const int units = halves ? a.d / 16 : a.d / 8;
     // as many heads per thread as leave eight waves a SIMD: the queries of a 32K
     // prompt (28 heads of 128, bf16) in 87 us there, 88 at 32 waves, 109 at 128
     const long long most = static_cast<long long>(cus > 0 ? cus : 256) * 2048;
@@ -278,13 +268,14 @@ hipError_t launch_rope(RopeArgs a, int cus, hipStream_t s) {
     a.hstep = static_cast<int>(hstep);
     const long long blocks = (tokens * units * hstep + kThreads - 1) / kThreads;
     const dim3 grid(static_cast<unsigned>(blocks));
-    if (vec && a.s[1].heads == 0) {
+    if (one) {
         const RopeStream& r = a.s[0];
         auto run = [&](auto in32, auto out32) {
-            if (a.interleaved)
-                k_rope_rows<decltype(in32)::value, decltype(out32)::value, true><<<grid, kThreads, 0, s>>>(a);
+            constexpr bool I = decltype(in32)::value, O = decltype(out32)::value;
+            if (halves)
+                k_rope_rows<I, O><<<grid, kThreads, 0, s>>>(a);
             else
-                k_rope_rows<decltype(in32)::value, decltype(out32)::value, false><<<grid, kThreads, 0, s>>>(a);
+                k_rope_any<I, O><<<grid, kThreads, 0, s>>>(a);
         };
         if (r.in32)
             r.out32 ? run(std::true_type{}, std::true_type{}) : run(std::true_type{}, std::false_type{});
@@ -292,10 +283,7 @@ hipError_t launch_rope(RopeArgs a, int cus, hipStream_t s) {
             r.out32 ? run(std::false_type{}, std::true_type{}) : run(std::false_type{}, std::false_type{});
         return hipGetLastError();
     }
-    if (vec)
-        k_rope<true><<<grid, kThreads, 0, s>>>(a);
-    else
-        k_rope<false><<<grid, kThreads, 0, s>>>(a);
+    k_rope<<<grid, kThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 

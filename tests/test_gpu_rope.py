@@ -82,6 +82,16 @@ def test_views_in_place_and_inverse():
            ref.rope_bound(one.cpu().expand(B, H, T, d), freqs.cpu(), F), "expanded")
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("d,rot,inter", [(128, 128, True), (128, 90, False), (64, 30, True), (64, 64, False)])
+def test_in_place_of_any_pairs(dtype, d, rot, inter):
+    x = _rand((2, 3, 70, d), dtype, rot).cuda()
+    freqs = sp.rope_frequencies(rot)
+    want = sp.rope(x, freqs, interleaved=inter, first=9)
+    assert sp.rope(x, freqs, interleaved=inter, first=9, out=x) is x
+    assert torch.equal(x, want)
+
+
 def test_gradient_is_the_rotation_back():
     """<g, d rope(x)> = <rope(g, -p), dx>: the gradient by the call with negated
     positions, against the formula's and against differences."""
