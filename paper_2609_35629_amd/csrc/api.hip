@@ -1413,8 +1413,8 @@ santapp_status santapp_prompt_attention(const santapp_score* score, const santap
     if (prefix && !causal) return fail(SANTAPP_EINVAL, "a prefix needs causal");
     if (!aligned4(documents) || !aligned4(prefix) || !aligned4(score->slopes))
         return fail(SANTAPP_EINVAL, "documents, prefix and slopes must be 4-byte aligned");
-    if ((causal || score->window > 0 || score->slopes || documents) &&
-        (offset < 0 || static_cast<long long>(offset) + T > N))
+    const bool placed = causal || score->window > 0 || score->slopes || documents;  // positions matter
+    if (placed && (offset < 0 || static_cast<long long>(offset) + T > N))
         return fail(SANTAPP_EINVAL, "queries %d .. %lld are not tokens of the sequence's %d", offset,
                     static_cast<long long>(offset) + T, N);
     if (T == 0) return ok();
@@ -1428,7 +1428,7 @@ santapp_status santapp_prompt_attention(const santapp_score* score, const santap
     }
     if (santapp_status st = check_apart(to, in, n)) return st;
     a.causal = causal != 0;
-    a.offset = offset;
+    a.offset = placed ? offset : 0;
     a.documents = documents;
     a.prefix = prefix;
     if (!aligned16(workspace)) return fail(SANTAPP_EINVAL, "workspace must be 16-byte aligned");

@@ -162,6 +162,12 @@ def test_future_keys_hold_anything():
     assert torch.equal(got.cpu().double(), want)
 
 
+@pytest.mark.parametrize("offset", [-(2 ** 31), 2 ** 31 - 1, 7])
+def test_without_masks_positions_do_not_matter(offset):
+    q, K = _rand((1, 2, 70, 64), BF, 1).cuda(), _rand((1, 1, 50, 64), BF, 2).cuda()
+    assert torch.equal(sp.prompt_attention(q, K, K, causal=False, offset=offset), sp.prompt_attention(q, K, K, causal=False))
+
+
 @pytest.mark.parametrize("dtype", [BF, F])
 def test_large_scores(dtype):
     # weights of one key; scores of thousands, and of every sign
