@@ -191,10 +191,9 @@ size_t plan_prefix(PrefixArgs& a, int cus, char* ws) {
     if (cus <= 0) cus = 256;
     const bool f32 = a.dtype == SANTAPP_FP32;
     const long long R = static_cast<long long>(a.S) * a.G, pairs = static_cast<long long>(a.P) * a.Hkv;
-    // blocks of 64 rows where 128 would leave more of the last one empty (64
-    // sequences of 7 heads: 448 rows)
+    // by rows alone: 448 rows (64 sequences of 7 heads) take 299 us in blocks of 128,
+    // an eighth of them empty, and 309 in full blocks of 64, over 131072 keys
     a.variant = variant_of(R);
-    if (a.variant == 2 && (R + 63) / 64 * 64 < (R + 127) / 128 * 128) a.variant = 1;
     const int bm = 32 * row_waves(a.variant), bk = tile_keys(a.variant, f32);
     const long long slots = static_cast<long long>(per_cu(a.variant, a.d, f32, f32 ? 1 : 3)) * cus;
     // the suffixes: a block per 32 heads (times the waves over rows) each, split
